@@ -328,6 +328,118 @@ paro_status paro_rotated_linear_mxfp4(const paro_rotation *rot, const paro_mxfp4
                                       const paro_half_t *X, int64_t ldx, paro_half_t *Y, int64_t ldy,
                                       int32_t T, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- Between the linears of a decoder layer: norm, positions, key-value cache, attention ----------
+ * What a program that serves tokens with the linears above needs next to them.  fp16 activations in
+ * rows as the linears read and write them (a head's channels lie side by side: head h of a row is its
+ * channels h*head_dim .. (h+1)*head_dim - 1, so the column ranges of one q/k/v linear's output can be
+ * passed as they are); fp32 arithmetic, one rounding at the store.  Row strides (ld*) are in elements,
+ * multiples of 8, and rows 16-byte aligned (PARO_ERR_ALIGN otherwise). */
+
+/* Root-mean-square norm with the residual's addition:
+ *      h = X + R (R NULL: h = X),   Y[t][c] = h[t][c] / sqrt(mean_c h[t][c]^2 + eps) * weight[c]
+ * The norm is taken of the unrounded fp32 h.  H (NULL: not wanted) receives h rounded to fp16.
+ * C a multiple of 8, at most 32768; weight: [C] fp16, 16-byte aligned.  H and Y may each be X or R
+ * itself (same row stride); H and Y must differ.  No workspace. */
+paro_status paro_rms_norm(const paro_half_t *X, int64_t ldx, const paro_half_t *R, int64_t ldr,
+                          const paro_half_t *weight, float eps, int32_t T, int32_t C, paro_half_t *H,
+                          int64_t ldh, paro_half_t *Y, int64_t ldy, void *stream);
+/* The same with the result in 8 bits: codes [T][C] in E4M3 (1-4-3 bits, bias 7, largest value 448, no
+ * infinities) and fp32 scales, one per row (group 0: [T]) or per `group` = 128 consecutive channels
+ * ([T][C/128], C a multiple of 128):  scale = max|y| / 448 (max|y| taken as 1e-30 at least),
+ * code = y / scale rounded to nearest even.  A value that is not finite gives the NaN code. */
+paro_status paro_rms_norm_quantize_e4m3(const paro_half_t *X, int64_t ldx, const paro_half_t *R, int64_t ldr,
+                                        const paro_half_t *weight, float eps, int32_t group, int32_t T,
+                                        int32_t C, paro_half_t *H, int64_t ldh, uint8_t *codes, float *scales,
+                                        void *stream);
+
+/* Rotary positions: the first rot_dim channels of every head are rot_dim/2 pairs (a, b), and pair i of
+ * a token at position p becomes
+ *      magnitude * (a cos(p f_i) - b sin(p f_i)),   magnitude * (a sin(p f_i) + b cos(p f_i)),   f = inv_freq
+ * The angle is reduced in fp64, so it is as exact as inv_freq at any 32-bit position. */
+typedef struct {
+    int32_t head_dim;         /* multiple of 16, at most 512                                    */
+    int32_t rot_dim;          /* multiple of 16, 16..head_dim                                   */
+    int32_t layout;           /* 0: pair i = channels (i, i + rot_dim/2); 1: channels (2i, 2i+1) */
+    float magnitude;          /* factor on the rotated channels (1: none)                       */
+    const float *inv_freq;    /* device [rot_dim/2], radians per position                       */
+} paro_rope_t;
+
+/* inv_freq (host, [rot_dim/2]) and magnitude of a model with frequencies base^(-2i/rot_dim), made for
+ * `trained` positions and used for `factor` (>= 1) times as many:
+ *   0  as they are (factor, trained, low, high are not looked at)
+ *   1  f / factor
+ *   2  a larger base: base * factor^(rot_dim / (rot_dim - 2))
+ *   3  by wavelength: with n = trained f / 2 pi turns over the trained length and s = clamp((n - low) /
+ *      (high - low), 0, 1):  s f + (1 - s) f / factor
+ *   4  by channel: c(n) = rot_dim ln(trained / (2 pi n)) / (2 ln base) is the (fractional) pair that makes n
+ *      turns; s = 1 - clamp((i - floor c(high)) / (ceil c(low) - floor c(high)), 0, 1), the bounds first
+ *      clamped to 0..rot_dim - 1 and kept at least 0.001 apart; s f + (1 - s) f / factor, and magnitude
+ *      0.1 ln(factor) + 1
+ * magnitude is 1 for 0..3.  low < high are turns (3: customarily 1 and 4; 4: 1 and 32).
+ * Host only.  PARO_ERR_NULL, PARO_ERR_SHAPE (rot_dim odd or < 2, base <= 1, factor < 1, trained < 1, low or
+ * high not positive or low >= high, scaling 2 with rot_dim 2), PARO_ERR_UNSUPPORTED (another scaling). */
+paro_status paro_rope_frequencies_host(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                       double trained, double low, double high, float *inv_freq_host,
+                                       float *magnitude_host);
+
+/* Y[t] = the T rows of X with every head's channels rotated; heads * rope->head_dim channels a row.
+ * positions: device [T].  Y == X (same ld) is allowed.  No workspace. */
+paro_status paro_rope(const paro_rope_t *rope, const paro_half_t *X, int64_t ldx, const int32_t *positions,
+                      int32_t heads, int32_t T, paro_half_t *Y, int64_t ldy, void *stream);
+
+/* A paged key-value cache.  Token slot n is place n % page of page n / page.  Keys are stored in units
+ * of 16 bytes that interleave the page's tokens (the operand order of the attention's matrix products);
+ * values a row per token.
+ *   format 0: fp16, k [n_pages][kv_heads][head_dim/8][page][8], v [n_pages][kv_heads][page][head_dim]
+ *   format 1: E4M3 codes, k [n_pages][kv_heads][head_dim/16][page][16], v [n_pages][kv_heads][page][head_dim],
+ *             and one scale byte per token and head, k_scale / v_scale [n_pages][kv_heads][page]: the code's
+ *             value counts 2^(byte - 127) times */
+typedef struct {
+    int32_t n_pages;
+    int32_t page;             /* tokens of a page: a power of two, 16..1024                     */
+    int32_t kv_heads;
+    int32_t head_dim;         /* 64, 128 or 256                                                 */
+    int32_t format;           /* 0: fp16, 1: E4M3                                               */
+    void *k, *v;              /* device, 16-byte aligned                                        */
+    uint8_t *k_scale, *v_scale; /* device, 4-byte aligned; NULL for format 0                     */
+} paro_kv_cache;
+
+/* The keys and values of T new tokens into their slots, and on the way the rotation of keys and queries.
+ * K, V: fp16 rows of kv_heads heads; slots: device [T], a negative slot, or one the cache does not have,
+ * leaves its token out of the cache (padding).  Slots of one call must differ.
+ * rope: NULL leaves queries and keys as they are (positions may be NULL then); rope->head_dim must be the
+ * cache's.  Q (NULL: none): rows of q_heads heads, rotated into Qr (Qr == Q, same ld, is allowed).
+ * Format 1: every (token, head) row takes the scale 2^e, the least e in -15..8 with max|row| <= 448 * 2^e, of the
+ * unrounded rotated row, and codes row / 2^e rounded to nearest even, those of e = 8 kept within 240 (larger
+ * ones would stand for values that fp16 does not have); values that are not finite become the NaN code and
+ * do not count for e.  All values a format-1 cache written by this call stands for are fp16 values.  No workspace. */
+paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rope_t *rope, const paro_half_t *K, int64_t ldk,
+                           const paro_half_t *V, int64_t ldv, const int64_t *slots, const int32_t *positions,
+                           int32_t T, const paro_half_t *Q, int64_t ldq, int32_t q_heads, paro_half_t *Qr,
+                           int64_t ldqr, void *stream);
+
+/* Attention of one new token of each of `batch` sequences over its cached tokens (its own among them):
+ *      O[b][h] = sum_t p_t v_t,   p = softmax over max(0, n - window) <= t < n of scale * q_h . k_t,   n = lengths[b]
+ * (window 0: all t < n).  Token t of sequence b is place t % page of page block_table[b * ld_table + t / page]
+ * (device int32 rows of table_width entries; entries past the sequence's pages are not looked at; ld_table 0
+ * shares one row).  Query head h reads key-value head h / (q_heads / kv_heads).  A sequence with nothing to
+ * attend to (n <= 0, or every score -inf) gives zeros and lse -inf; n beyond the table is taken as the
+ * table's end; tokens of a page the cache does not have are left out.  Cache places past n do not matter,
+ * whatever they hold.  lse (NULL: not wanted): fp32 [batch][q_heads], ln sum_t exp(scale q . k_t).
+ * Q, O: fp16 rows of q_heads heads of head_dim; q_heads a multiple of kv_heads.  scale must be finite.
+ * ws: >= paro_workspace_bytes_attention() bytes, 256-byte aligned, in the two parts described at
+ * paro_workspace_bytes(): the exchange part (paro_workspace_exchange_bytes_attention(), zero-filled once,
+ * all zero again after every call) counts arrivals, the scratch part at the buffer's end holds fp32 partial
+ * results of sequences that several blocks share.  Blocks never wait for each other.  A buffer may be
+ * shared with the linear calls under the rule given there.  Results do not depend on timing. */
+size_t paro_workspace_exchange_bytes_attention(const paro_kv_cache *cache, int32_t q_heads, int32_t batch);
+size_t paro_workspace_bytes_attention(const paro_kv_cache *cache, int32_t q_heads, int32_t batch);
+paro_status paro_paged_attention(const paro_kv_cache *cache, const paro_half_t *Q, int64_t ldq, int32_t q_heads,
+                                 const int32_t *block_table, int64_t ld_table, int32_t table_width,
+                                 const int32_t *lengths, int32_t batch, float scale, int32_t window,
+                                 paro_half_t *O, int64_t ldo, float *lse, void *ws, size_t ws_bytes,
+                                 void *stream);
+
 /* Test hooks for the bit-exact gate --------------------------------------------------- */
 
 /* codes[n][c] = q[n, c] as bytes 0..15 (from w->packed if set, else from w->qweight). */

@@ -47,6 +47,18 @@ class _CMxfp4Weight(ctypes.Structure):
     ]
 
 
+class _CRope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p)]
+
+
+class _CKVCache(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -104,6 +116,17 @@ def lib():
         L.paro_workspace_bytes_mxfp4.restype = sz
         L.paro_workspace_bytes_mxfp4.argtypes = [i32, i32]
         L.paro_rotated_linear_mxfp4.argtypes = [rp, mp, vp, i64, vp, i64, i32, vp, sz, vp]
+        f32, f64, hp, cp = ctypes.c_float, ctypes.c_double, ctypes.POINTER(_CRope), ctypes.POINTER(_CKVCache)
+        L.paro_rms_norm.argtypes = [vp, i64, vp, i64, vp, f32, i32, i32, vp, i64, vp, i64, vp]
+        L.paro_rms_norm_quantize_e4m3.argtypes = [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, vp, vp]
+        L.paro_rope_frequencies_host.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, vp]
+        L.paro_rope.argtypes = [hp, vp, i64, vp, i32, i32, vp, i64, vp]
+        L.paro_kv_append.argtypes = [cp, hp, vp, i64, vp, i64, vp, vp, i32, vp, i64, i32, vp, i64, vp]
+        L.paro_workspace_exchange_bytes_attention.restype = sz
+        L.paro_workspace_exchange_bytes_attention.argtypes = [cp, i32, i32]
+        L.paro_workspace_bytes_attention.restype = sz
+        L.paro_workspace_bytes_attention.argtypes = [cp, i32, i32]
+        L.paro_paged_attention.argtypes = [cp, vp, i64, i32, vp, i64, i32, vp, i32, f32, i32, vp, i64, vp, vp, sz, vp]
         L.paro_diag_read_stream.argtypes = [vp, sz, vp, i32, vp]
         L.paro_diag_mfma_f16.argtypes = [vp, sz, i32, i32, i32, vp]
         L.paro_diag_mfma_f16_flops.argtypes = [i32, i32]
@@ -117,7 +140,8 @@ def lib():
                      "paro_w4_dequant", "paro_w4_quantize", "paro_rotated_linear_multi",
                      "paro_rotate_scale_quantize_int4", "paro_rotate_scale_quantize_mxfp4",
                      "paro_diag_read_stream", "paro_diag_mfma_f16", "paro_fwht", "paro_mxfp4_quantize_weight",
-                     "paro_mxfp4_repack", "paro_mxfp4_unpack", "paro_mxfp4_linear", "paro_rotated_linear_mxfp4"):
+                     "paro_mxfp4_repack", "paro_mxfp4_unpack", "paro_mxfp4_linear", "paro_rotated_linear_mxfp4", "paro_rms_norm",
+                     "paro_rms_norm_quantize_e4m3", "paro_rope_frequencies_host", "paro_rope", "paro_kv_append", "paro_paged_attention"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -146,6 +170,77 @@ class _CtypesCalls:
         st = lib().paro_rotate_scale(ctypes.byref(rot), X.data_ptr(), ldx, Xr.data_ptr(), ldxr, T, _stream())
         return Xr if st == PARO_OK else st
 
+    @staticmethod
+    def rms_norm(X, w, eps, R, Y, H):
+        ldx = _gpu_rows(X)
+        T, C = X.shape
+        _gpu_vector(w, torch.float16, C)
+        ldr = 0 if R is None else _gpu_rows(R, T, C)
+        Y, ldy = _rows_or_new(Y, T, C, X)
+        H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
+        st = lib().paro_rms_norm(X.data_ptr(), ldx, _ptr(R), ldr, w.data_ptr(), eps, T, C, _ptr(H), ldh, Y.data_ptr(), ldy, _stream())
+        return st if st != PARO_OK else Y if R is None else (Y, H)
+
+    @staticmethod
+    def rms_norm_quantize_e4m3(X, w, eps, group, R, H):
+        ldx = _gpu_rows(X)
+        T, C = X.shape
+        _gpu_vector(w, torch.float16, C)
+        ldr = 0 if R is None else _gpu_rows(R, T, C)
+        H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
+        codes = torch.empty((T, C), dtype=torch.uint8, device=X.device)
+        scales = torch.empty((T, C // group if group > 0 else 1), dtype=torch.float32, device=X.device)
+        st = lib().paro_rms_norm_quantize_e4m3(X.data_ptr(), ldx, _ptr(R), ldr, w.data_ptr(), eps, group, T, C, _ptr(H), ldh, codes.data_ptr(),
+                                               scales.data_ptr(), _stream())
+        return st if st != PARO_OK else (codes, scales) if R is None else (codes, scales, H)
+
+    @staticmethod
+    def rope(rope, X, positions, Y):
+        ldx = _gpu_rows(X)
+        T, C = X.shape
+        _gpu_vector(positions, torch.int32, T)
+        assert C % rope.head_dim == 0, "rows are not whole heads"
+        Y, ldy = _rows_or_new(Y, T, C, X)
+        st = lib().paro_rope(ctypes.byref(rope), X.data_ptr(), ldx, positions.data_ptr(), C // rope.head_dim, T, Y.data_ptr(), ldy, _stream())
+        return Y if st == PARO_OK else st
+
+    @staticmethod
+    def kv_append(cache, rope, K, V, slots, positions, Q, Qr):
+        width = cache.kv_heads * cache.head_dim
+        ldk = _gpu_rows(K, -1, width)
+        T = K.shape[0]
+        ldv = _gpu_rows(V, T, width)
+        _gpu_vector(slots, torch.int64, T)
+        if positions is not None:
+            _gpu_vector(positions, torch.int32, T)
+        ldq = ldqr = heads = 0
+        if Q is not None:
+            ldq = _gpu_rows(Q, T)
+            assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
+            heads = Q.shape[1] // cache.head_dim
+            Qr, ldqr = _rows_or_new(Qr, T, Q.shape[1], Q)
+        else:
+            Qr = None
+        st = lib().paro_kv_append(ctypes.byref(cache), None if rope is None else ctypes.byref(rope), K.data_ptr(), ldk, V.data_ptr(), ldv,
+                                  slots.data_ptr(), _ptr(positions), T, _ptr(Q), ldq, heads, _ptr(Qr), ldqr, _stream())
+        return Qr if st == PARO_OK else st
+
+    @staticmethod
+    def paged_attention(cache, Q, table, lengths, buf, nbytes, scale, window, O, with_lse):
+        ldq = _gpu_rows(Q)
+        B = Q.shape[0]
+        assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
+        assert table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.shape[0] == B and table.is_cuda
+        _gpu_vector(lengths, torch.int32, B)
+        assert buf.is_cuda
+        heads = Q.shape[1] // cache.head_dim
+        O, ldo = _rows_or_new(O, B, Q.shape[1], Q)
+        lse = torch.empty((B, heads), dtype=torch.float32, device=Q.device) if with_lse else None
+        st = lib().paro_paged_attention(ctypes.byref(cache), Q.data_ptr(), ldq, heads, table.data_ptr(), table.shape[1] if B == 1 else table.stride(0),
+                                        table.shape[1], lengths.data_ptr(), B, scale, window, O.data_ptr(), ldo, _ptr(lse), buf.data_ptr(), nbytes,
+                                        _stream())
+        return st if st != PARO_OK else (O, lse) if with_lse else O
+
 
 def _native():
     """The native half of the linear calls (csrc/host_call.cpp), over the same libparo.so; where it is not built, or was built
@@ -156,6 +251,7 @@ def _native():
         try:
             from . import paro_host
             paro_host.types(_CRotation, _CW4Weight)
+            paro_host.token_types(_CRope, _CKVCache)
             _host = paro_host
         except ImportError as e:
             if os.path.exists(_HOST_PATH):
@@ -326,12 +422,16 @@ class Workspace:
         return hi <= lo or int(self.buf[lo:hi].max().item()) == 0
 
     @classmethod
-    def shared(cls, calls, device="cuda"):
-        """One workspace for calls of several shapes: calls = [(rot or None, weight, T), ...].  Sized as the
-        largest exchange part plus the largest scratch part, so no call's scratch touches another's exchange part."""
+    def shared(cls, calls, device="cuda", attention=()):
+        """One workspace for calls of several shapes: calls = [(rot or None, weight, T), ...], attention = [(cache, q_heads,
+        batch), ...].  Sized as the largest exchange part plus the largest scratch part, so no call's scratch touches
+        another's exchange part."""
         ex = sc = 0
         for rot, w, T in calls:
             total, e = paro_workspace_bytes(rot, w, T), paro_workspace_exchange_bytes(rot, w, T)
+            ex, sc = max(ex, e), max(sc, total - e)
+        for call in attention:
+            total, e = paro_workspace_bytes_attention(*call), paro_workspace_exchange_bytes_attention(*call)
             ex, sc = max(ex, e), max(sc, total - e)
         ws = cls(ex + sc, device)
         ws.exchange_bytes = ex
@@ -382,6 +482,25 @@ def paro_workspace_exchange_bytes(rot: Rotation | None, w: W4Weight, T: int) -> 
 def _rows(x: torch.Tensor):
     assert x.dtype == torch.float16 and x.dim() == 2 and x.stride(1) == 1
     return x.shape[0], x.stride(0)
+
+
+def _gpu_rows(x: torch.Tensor, T: int = -1, width: int | None = None) -> int:
+    """The row stride of fp16 rows on the GPU, checked as the native calls check them."""
+    rows, ld = _rows(x)
+    assert x.is_cuda, "expected a tensor on the GPU"
+    assert (T < 0 or rows == T) and (width is None or x.shape[1] == width), "tensors of different shapes"
+    return ld
+
+
+def _gpu_vector(x: torch.Tensor, dtype, n: int) -> None:
+    assert x.dtype == dtype and x.dim() == 1 and x.is_contiguous() and x.shape[0] == n, "expected a contiguous vector of another type or length"
+    assert x.is_cuda, "expected a tensor on the GPU"
+
+
+def _rows_or_new(x, T: int, width: int, like: torch.Tensor):
+    if x is None:
+        return torch.empty((T, width), dtype=torch.float16, device=like.device), width
+    return x, _gpu_rows(x, T, width)
 
 
 def paro_rotate_scale(rot: Rotation, X: torch.Tensor, Xr: torch.Tensor | None = None) -> torch.Tensor:
@@ -559,3 +678,106 @@ def paro_rotated_linear_mxfp4(rot: Rotation, w: Mxfp4Weight, X: torch.Tensor, ws
     _check(lib().paro_rotated_linear_mxfp4(rot.ref(), w.ref(), X.data_ptr(), ldx, Y.data_ptr(), ldy, T, ws.data_ptr(),
                                            ws.numel(), _stream()), "paro_rotated_linear_mxfp4")
     return Y
+
+
+# ---- Between the linears of a decoder layer ------------------------------------------------------------------------------
+
+def paro_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None, Y: torch.Tensor | None = None,
+                  H: torch.Tensor | None = None):
+    """RMS norm of X + residual: Y, or (Y, H) with a residual, H being the sum (Y and H may be X or residual themselves)."""
+    return _output((_host or _native()).rms_norm(X, weight, eps, residual, Y, H), "paro_rms_norm")
+
+
+def paro_rms_norm_quantize_e4m3(X: torch.Tensor, weight: torch.Tensor, eps: float, group: int = 0, residual: torch.Tensor | None = None,
+                                H: torch.Tensor | None = None):
+    """The same in 8 bits: (codes uint8 [T][C] of E4M3, scales fp32 [T][1] or, with group 128, [T][C/128]), and H with a residual."""
+    return _output((_host or _native()).rms_norm_quantize_e4m3(X, weight, eps, group, residual, H), "paro_rms_norm_quantize_e4m3")
+
+
+ROPE_LAYOUTS = {"halves": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3, "channels": 4}
+
+
+def paro_rope_frequencies_host(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: float = 0.0,
+                               low: float = 1.0, high: float = 4.0):
+    """(radians per position of every pair as numpy fp32, magnitude); the scalings are those of paro_rope_frequencies_host in paro.h."""
+    f, m = np.empty(max(rot_dim // 2, 1), dtype=np.float32), np.empty(1, dtype=np.float32)
+    _check(lib().paro_rope_frequencies_host(rot_dim, base, ROPE_SCALINGS[scaling], factor, trained, low, high, f.ctypes.data, m.ctypes.data),
+           "paro_rope_frequencies_host")
+    return f, float(m[0])
+
+
+class Rope:
+    """Rotary positions of heads (struct paro_rope_t): inv_freq fp32 [rot_dim/2] (tensor or array), the first rot_dim channels rotated."""
+
+    def __init__(self, inv_freq, head_dim: int, layout: str = "halves", magnitude: float = 1.0, device="cuda"):
+        if not isinstance(inv_freq, torch.Tensor):
+            inv_freq = torch.as_tensor(np.ascontiguousarray(inv_freq, dtype=np.float32)).to(device)
+        assert inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()
+        self.inv_freq, self.head_dim, self.rot_dim = inv_freq, head_dim, 2 * inv_freq.shape[0]
+        self.c = _CRope(head_dim, self.rot_dim, ROPE_LAYOUTS[layout], magnitude, _ptr(inv_freq))
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def paro_rope(rope: Rope, X: torch.Tensor, positions: torch.Tensor, Y: torch.Tensor | None = None) -> torch.Tensor:
+    """Rows of heads rotated to int32 positions [T]; Y may be X."""
+    return _output((_host or _native()).rope(rope.c, X, positions, Y), "paro_rope")
+
+
+class KVCache:
+    """A paged key-value cache on the device (struct paro_kv_cache), "fp16" or "e4m3".  Keys: [n_pages][kv_heads][head_dim/u][page][u], u the
+    channels of 16 bytes; values [n_pages][kv_heads][page][head_dim]; e4m3 adds scale bytes [n_pages][kv_heads][page] to either."""
+
+    def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page: int = 16, format: str = "fp16", device="cuda"):
+        dtype, u = {"fp16": (torch.float16, 8), "e4m3": (torch.uint8, 16)}[format]
+        k = torch.zeros((n_pages, kv_heads, head_dim // u, page, u), dtype=dtype, device=device)
+        v = torch.zeros((n_pages, kv_heads, page, head_dim), dtype=dtype, device=device)
+        scales = [torch.full((n_pages, kv_heads, page), 127, dtype=torch.uint8, device=device) for _ in range(2)] if u == 16 else (None, None)
+        self._take(k, v, *scales)
+
+    @classmethod
+    def from_device(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        """Wrap tensors in the cache's layout that already live on the device."""
+        self = cls.__new__(cls)
+        self._take(k, v, k_scale, v_scale)
+        return self
+
+    def _take(self, k, v, k_scale, v_scale):
+        e4m3 = k_scale is not None
+        self.n_pages, self.kv_heads, self.page, self.head_dim = v.shape
+        u = 16 if e4m3 else 8
+        assert k.dtype == v.dtype == (torch.uint8 if e4m3 else torch.float16) and k.is_contiguous() and v.is_contiguous()
+        assert k.shape == (self.n_pages, self.kv_heads, self.head_dim // u, self.page, u)
+        for s in (k_scale, v_scale) if e4m3 else ():
+            assert s.dtype == torch.uint8 and s.is_contiguous() and s.shape == (self.n_pages, self.kv_heads, self.page)
+        self.format = "e4m3" if e4m3 else "fp16"
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = _CKVCache(self.n_pages, self.page, self.kv_heads, self.head_dim, int(e4m3), _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def paro_kv_append(cache: KVCache, K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, rope: Rope | None = None,
+                   positions: torch.Tensor | None = None, Q: torch.Tensor | None = None, Qr: torch.Tensor | None = None):
+    """K and V rows into their slots (int64 [T], negative: left out), keys and queries rotated on the way; returns the rotated queries, if any."""
+    return _output((_host or _native()).kv_append(cache.c, None if rope is None else rope.c, K, V, slots, positions, Q, Qr), "paro_kv_append")
+
+
+def paro_workspace_bytes_attention(cache: KVCache, q_heads: int, batch: int) -> int:
+    return lib().paro_workspace_bytes_attention(cache.ref(), q_heads, batch)
+
+
+def paro_workspace_exchange_bytes_attention(cache: KVCache, q_heads: int, batch: int) -> int:
+    return lib().paro_workspace_exchange_bytes_attention(cache.ref(), q_heads, batch)
+
+
+def paro_paged_attention(cache: KVCache, Q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, ws: Workspace,
+                         scale: float | None = None, window: int = 0, O: torch.Tensor | None = None, with_lse: bool = False):
+    """One new token of every sequence against its cached ones (int32 block_table [B][pages], lengths [B]): O, or (O, lse fp32 [B][q_heads])."""
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    return _output((_host or _native()).paged_attention(cache.c, Q, block_table, lengths, ws.buf, ws.nbytes, scale, window, O, with_lse),
+                   "paro_paged_attention")

@@ -1,4 +1,4 @@
-// The linear calls of binding.py in one native step: checks on the tensors, the output, the current stream and the library
+// The linear calls of binding.py, and those of a token's way between linears, in one native step: checks on the tensors, the output, the current stream and the library
 // call.  One token through a 512 -> 512 linear, called eagerly, is bound by the host: in Python the same steps took 3.4 us beside
 // the 3.3 of the call itself (the output alone 1.7, the checks of rows and strides 0.5, the stream's handle 0.4).
 #include <Python.h>
@@ -12,7 +12,7 @@
 namespace {
 
 // The ctypes classes of the two structures (binding.py hands them over once).
-PyObject *g_rotation, *g_weight;
+PyObject *g_rotation, *g_weight, *g_rope, *g_cache;
 
 // A ctypes structure of class `type` through the buffer protocol; NULL with an exception set if it is anything else.
 template <class T>
@@ -29,14 +29,16 @@ const T *structure(PyObject *o, PyObject *type)
     return (const T *)p;
 }
 
-PyObject *types(PyObject *, PyObject *const *a, Py_ssize_t n)
+PyObject *keep_types(PyObject *const *a, Py_ssize_t n, PyObject *&first, PyObject *&second)
 {
     if (n != 2 || !PyType_Check(a[0]) || !PyType_Check(a[1])) { PyErr_SetString(PyExc_TypeError, "types takes two classes"); return nullptr; }
     Py_INCREF(a[0]); Py_INCREF(a[1]);
-    Py_XDECREF(g_rotation); Py_XDECREF(g_weight);
-    g_rotation = a[0]; g_weight = a[1];
+    Py_XDECREF(first); Py_XDECREF(second);
+    first = a[0]; second = a[1];
     Py_RETURN_NONE;
 }
+PyObject *types(PyObject *, PyObject *const *a, Py_ssize_t n) { return keep_types(a, n, g_rotation, g_weight); }
+PyObject *token_types(PyObject *, PyObject *const *a, Py_ssize_t n) { return keep_types(a, n, g_rope, g_cache); }
 
 const at::Tensor *tensor(PyObject *o)
 {
@@ -125,10 +127,200 @@ PyObject *rotate(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- Between the linears ---------------------------------------------------------------------------------------------
+
+bool refuse(const char *why)
+{
+    PyErr_SetString(PyExc_AssertionError, why);
+    return false;
+}
+
+// fp16 rows of `width` channels on the GPU; `t` tokens (-1: any)
+bool gpu_rows(const at::Tensor &x, int64_t t, int64_t width)
+{
+    if (!rows(x)) return false;
+    if (!x.is_cuda()) return refuse("expected a tensor on the GPU");
+    if ((t >= 0 && x.size(0) != t) || x.size(1) != width) return refuse("tensors of different shapes");
+    return true;
+}
+bool gpu_vector(const at::Tensor &x, at::ScalarType type, int64_t n)
+{
+    if (x.scalar_type() != type || x.dim() != 1 || !x.is_contiguous() || x.size(0) != n) return refuse("expected a contiguous vector of another type or length");
+    return x.is_cuda() || refuse("expected a tensor on the GPU");
+}
+// An optional tensor argument; false with an exception set if it is anything else.
+bool maybe(PyObject *o, const at::Tensor *&t)
+{
+    t = nullptr;
+    return o == Py_None || (t = tensor(o));
+}
+// `o` if given, else new rows; undefined with an exception set on failure
+at::Tensor rows_or_new(PyObject *o, int64_t t, int64_t width, const at::Tensor &like)
+{
+    if (o == Py_None) return at::empty({t, width}, like.options().requires_grad(false));
+    const at::Tensor *x = tensor(o);
+    return x && gpu_rows(*x, t, width) ? *x : at::Tensor();
+}
+const paro_half_t *half_ptr(const at::Tensor *t) { return t ? (const paro_half_t *)t->data_ptr() : nullptr; }
+paro_half_t *half_out(const at::Tensor &t) { return (paro_half_t *)t.data_ptr(); }
+void *current_stream() { return (void *)c10::hip::getCurrentHIPStream().stream(); }
+PyObject *wrap(PyObject *given, at::Tensor &&t)
+{
+    if (given != Py_None) { Py_INCREF(given); return given; }
+    return THPVariable_Wrap(std::move(t));
+}
+PyObject *together(std::initializer_list<PyObject *> parts)
+{
+    PyObject *out = PyTuple_New((Py_ssize_t)parts.size());
+    Py_ssize_t i = 0;
+    for (PyObject *p : parts) {
+        if (!p || !out) { Py_XDECREF(p); continue; }
+        PyTuple_SET_ITEM(out, i++, p);
+    }
+    if (out && i == (Py_ssize_t)parts.size()) return out;
+    Py_XDECREF(out);
+    return nullptr;
+}
+
+// rms_norm(X, weight, eps, residual or None, Y or None, H or None) -> Y, or (Y, H) with a residual
+PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) { PyErr_SetString(PyExc_TypeError, "rms_norm takes 6 arguments"); return nullptr; }
+    const at::Tensor *x = tensor(a[0]), *w = x ? tensor(a[1]) : nullptr, *r;
+    if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*w, at::kHalf, x->size(1))) return nullptr;
+    const float eps = (float)PyFloat_AsDouble(a[2]);
+    const int64_t T = x->size(0), C = x->size(1);
+    if (PyErr_Occurred() || !maybe(a[3], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    at::Tensor y = rows_or_new(a[4], T, C, *x), h;
+    if (!y.defined()) return nullptr;
+    if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
+    const paro_status st = paro_rms_norm(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, (int32_t)T, (int32_t)C,
+                                         r ? half_out(h) : nullptr, r ? h.stride(0) : 0, half_out(y), y.stride(0), current_stream());
+    if (st != PARO_OK) return PyLong_FromLong(st);
+    PyObject *first = wrap(a[4], std::move(y));
+    return r ? together({first, wrap(a[5], std::move(h))}) : first;
+    END_HANDLE_TH_ERRORS
+}
+
+// rms_norm_quantize_e4m3(X, weight, eps, group, residual or None, H or None) -> (codes, scales), or (codes, scales, H) with a residual
+PyObject *rms_norm_quantize_e4m3(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 6) { PyErr_SetString(PyExc_TypeError, "rms_norm_quantize_e4m3 takes 6 arguments"); return nullptr; }
+    const at::Tensor *x = tensor(a[0]), *w = x ? tensor(a[1]) : nullptr, *r;
+    if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*w, at::kHalf, x->size(1))) return nullptr;
+    const float eps = (float)PyFloat_AsDouble(a[2]);
+    const int32_t group = (int32_t)PyLong_AsLong(a[3]);
+    const int64_t T = x->size(0), C = x->size(1);
+    if (PyErr_Occurred() || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    at::Tensor h;
+    if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
+    at::Tensor codes = at::empty({T, C}, x->options().dtype(at::kByte).requires_grad(false));
+    at::Tensor scales = at::empty({T, group > 0 ? C / group : 1}, x->options().dtype(at::kFloat).requires_grad(false));
+    const paro_status st = paro_rms_norm_quantize_e4m3(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, group, (int32_t)T,
+                                                       (int32_t)C, r ? half_out(h) : nullptr, r ? h.stride(0) : 0, (uint8_t *)codes.data_ptr(),
+                                                       (float *)scales.data_ptr(), current_stream());
+    if (st != PARO_OK) return PyLong_FromLong(st);
+    PyObject *first = THPVariable_Wrap(std::move(codes)), *second = THPVariable_Wrap(std::move(scales));
+    return r ? together({first, second, wrap(a[5], std::move(h))}) : together({first, second});
+    END_HANDLE_TH_ERRORS
+}
+
+// rope(rope, X, positions, Y or None)
+PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 4) { PyErr_SetString(PyExc_TypeError, "rope takes 4 arguments"); return nullptr; }
+    const paro_rope_t *rp = structure<paro_rope_t>(a[0], g_rope);
+    const at::Tensor *x = rp ? tensor(a[1]) : nullptr, *at_ = x ? tensor(a[2]) : nullptr;
+    if (!at_ || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*at_, at::kInt, x->size(0))) return nullptr;
+    const int64_t T = x->size(0), C = x->size(1);
+    if (rp->head_dim <= 0 || C % rp->head_dim) { refuse("rows are not whole heads"); return nullptr; }
+    at::Tensor y = rows_or_new(a[3], T, C, *x);
+    if (!y.defined()) return nullptr;
+    const paro_status st = paro_rope(rp, half_ptr(x), x->stride(0), (const int32_t *)at_->data_ptr(), (int32_t)(C / rp->head_dim), (int32_t)T,
+                                     half_out(y), y.stride(0), current_stream());
+    return st != PARO_OK ? PyLong_FromLong(st) : wrap(a[3], std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_append(cache, rope or None, K, V, slots, positions or None, Q or None, Qr or None) -> Qr, or None without Q
+PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8) { PyErr_SetString(PyExc_TypeError, "kv_append takes 8 arguments"); return nullptr; }
+    const paro_kv_cache *c = structure<paro_kv_cache>(a[0], g_cache);
+    const paro_rope_t *rp = !c || a[1] == Py_None ? nullptr : structure<paro_rope_t>(a[1], g_rope);
+    if (!c || (!rp && a[1] != Py_None)) return nullptr;
+    const at::Tensor *k = tensor(a[2]), *v = k ? tensor(a[3]) : nullptr, *slots = v ? tensor(a[4]) : nullptr, *at_, *q;
+    if (!slots || !maybe(a[5], at_) || !maybe(a[6], q)) return nullptr;
+    const int64_t width = (int64_t)c->kv_heads * c->head_dim;
+    if (!rows(*k) || !gpu_rows(*k, -1, width) || !gpu_rows(*v, k->size(0), width)) return nullptr;
+    const int64_t T = k->size(0);
+    if (!gpu_vector(*slots, at::kLong, T) || (at_ && !gpu_vector(*at_, at::kInt, T))) return nullptr;
+    at::Tensor out;
+    int64_t heads = 0;
+    if (q) {
+        if (!rows(*q) || !gpu_rows(*q, T, q->size(1))) return nullptr;
+        if (c->head_dim <= 0 || q->size(1) % c->head_dim) { refuse("rows are not whole heads"); return nullptr; }
+        heads = q->size(1) / c->head_dim;
+        if (!(out = rows_or_new(a[7], T, q->size(1), *q)).defined()) return nullptr;
+    }
+    const paro_status st = paro_kv_append(c, rp, half_ptr(k), k->stride(0), half_ptr(v), v->stride(0), (const int64_t *)slots->data_ptr(),
+                                          at_ ? (const int32_t *)at_->data_ptr() : nullptr, (int32_t)T, half_ptr(q), q ? q->stride(0) : 0,
+                                          (int32_t)heads, q ? half_out(out) : nullptr, q ? out.stride(0) : 0, current_stream());
+    if (st != PARO_OK) return PyLong_FromLong(st);
+    if (!q) Py_RETURN_NONE;
+    return wrap(a[7], std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_attention(cache, Q, block_table, lengths, workspace, bytes, scale, window, O or None, with_lse) -> O, or (O, lse)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 10) { PyErr_SetString(PyExc_TypeError, "paged_attention takes 10 arguments"); return nullptr; }
+    const paro_kv_cache *c = structure<paro_kv_cache>(a[0], g_cache);
+    const at::Tensor *q = c ? tensor(a[1]) : nullptr, *table = q ? tensor(a[2]) : nullptr, *lengths = table ? tensor(a[3]) : nullptr;
+    const at::Tensor *ws = lengths ? tensor(a[4]) : nullptr;
+    if (!ws || !rows(*q) || !gpu_rows(*q, -1, q->size(1))) return nullptr;
+    const int64_t B = q->size(0);
+    if (c->head_dim <= 0 || q->size(1) % c->head_dim) { refuse("rows are not whole heads"); return nullptr; }
+    if (table->scalar_type() != at::kInt || table->dim() != 2 || (table->stride(1) != 1 && table->size(1) != 1) || table->size(0) != B || !table->is_cuda()) {
+        refuse("expected a block table of int32 rows on the GPU, one per sequence");
+        return nullptr;
+    }
+    if (!gpu_vector(*lengths, at::kInt, B)) return nullptr;
+    if (!ws->is_cuda()) { refuse("expected a tensor on the GPU"); return nullptr; }
+    const size_t bytes = PyLong_AsSize_t(a[5]);
+    const float scale = (float)PyFloat_AsDouble(a[6]);
+    const int32_t window = (int32_t)PyLong_AsLong(a[7]);
+    const int want = PyObject_IsTrue(a[9]);
+    if (PyErr_Occurred() || want < 0) return nullptr;
+    const int64_t heads = q->size(1) / c->head_dim, ld = B == 1 ? table->size(1) : table->stride(0);
+    at::Tensor o = rows_or_new(a[8], B, q->size(1), *q), lse;
+    if (!o.defined()) return nullptr;
+    if (want) lse = at::empty({B, heads}, q->options().dtype(at::kFloat).requires_grad(false));
+    const paro_status st = paro_paged_attention(c, half_ptr(q), q->stride(0), (int32_t)heads, (const int32_t *)table->data_ptr(), ld,
+                                                (int32_t)table->size(1), (const int32_t *)lengths->data_ptr(), (int32_t)B, scale, window, half_out(o),
+                                                o.stride(0), want ? (float *)lse.data_ptr() : nullptr, ws->data_ptr(), bytes, current_stream());
+    if (st != PARO_OK) return PyLong_FromLong(st);
+    PyObject *first = wrap(a[8], std::move(o));
+    return want ? together({first, THPVariable_Wrap(std::move(lse))}) : first;
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"types", (PyCFunction)(void (*)(void))types, METH_FASTCALL, nullptr},
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, nullptr},
     {"rotate", (PyCFunction)(void (*)(void))rotate, METH_FASTCALL, nullptr},
+    {"token_types", (PyCFunction)(void (*)(void))token_types, METH_FASTCALL, nullptr},
+    {"rms_norm", (PyCFunction)(void (*)(void))rms_norm, METH_FASTCALL, nullptr},
+    {"rms_norm_quantize_e4m3", (PyCFunction)(void (*)(void))rms_norm_quantize_e4m3, METH_FASTCALL, nullptr},
+    {"rope", (PyCFunction)(void (*)(void))rope, METH_FASTCALL, nullptr},
+    {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, nullptr},
+    {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "paro_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
