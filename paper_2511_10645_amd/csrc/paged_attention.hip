@@ -5,12 +5,13 @@
 // Bound by HBM: 2 head_dim elements per token and key-value head are read once and used for q_heads / kv_heads
 // queries, a few flops per byte.
 //
-// Work is cut into units of 32 tokens of one (sequence, key-value head, 16 of its query heads), numbered one
-// sequence after the other, and every block takes the same number of consecutive units, whatever the lengths are: a
-// block finds its place from a sum over the lengths.  The 4 waves of a block take its units in turn, each with a
-// running maximum of its own, and join through LDS where a sequence's head ends; heads that several blocks share leave
-// fp32 partial results in the scratch, and the block that arrives last (a counter per head; nobody waits) joins them in
-// the order of their units, so that results do not depend on timing.
+// Work is cut into units of 32 tokens of one (sequence, key-value head, up to 16 of its query heads) - a segment being
+// all units of such a head - numbered one sequence after the other, and every wave of the grid takes the same number of
+// consecutive units, whatever the lengths are: it finds its place from a sum over the lengths.  A wave writes the
+// results of segments that are all its own; shares of others go to LDS, where the block's waves join them, and
+// segments that several blocks share leave fp32 partial results in the scratch, joined by the block that arrives last
+// (a counter per segment; nobody waits) in the order of their units, so that results do not depend on timing.  More than
+// kGroupParts of them are joined in groups first, each by the last block of its group.
 //
 // A wave multiplies on the matrix cores without LDS: keys are the A operand of S^T = K Q^T (the cache keeps them in
 // that operand's order, so a request of 64 lanes is contiguous), and S^T leaves the instruction as the B operand
@@ -27,14 +28,24 @@
 namespace paro {
 
 constexpr int kUnit = 32;                        // tokens of a unit
-constexpr int kAttnWaves = 4;
-constexpr int kAttnBlocks = 512;                 // most blocks of a launch: 2 for every compute unit
+constexpr int kAttnBlocks = 256;                 // most blocks of a launch: one for every compute unit
 constexpr int kQueries = 16;                     // query heads of a unit: the N of the matrix instruction
+constexpr int kGroupParts = 32;                  // partial results that are joined at once
 constexpr float kPShift = 15.0f;                 // p is held 2^15 times
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kRsrcRaw = 0x00020000;             // raw buffer, 32-bit data format
+constexpr int kAgent = 16;                       // agent scope: past the L2 of the XCD
+#ifndef STREAM_AUX
+#define STREAM_AUX 2
+#endif
+constexpr int kOnce = STREAM_AUX;                         // keys and values are read once: non-temporal
 
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+
+// waves of a block: two for every SIMD, one where a wave's registers are more than half of them
+template <int D> constexpr int attn_waves() { return D == 256 ? 4 : 8; }
 
 struct AttnArgs {
     const uint8_t *k, *v, *ks, *vs;
@@ -42,44 +53,56 @@ struct AttnArgs {
     const int32_t *table, *lengths;
     _Float16 *o;
     float *lse;
-    uint32_t *arrived;                           // [batch][kv_heads * chunks]
-    float *partial;                              // [2 * blocks][kQueries * (D + 2)]
+    uint32_t *arrived;                           // [2 * kAttnBlocks] of groups of parts, [batch][kv_heads * chunks] of segments
+    float *partial;                              // [2 * kAttnBlocks][kQueries * (D + 4)]: m, l, then the row, of every query
     int64_t ldq, ldo, ld_table;
     int page_log, n_pages, kv_heads, group, chunks, width, batch, window;
     float scale;                                 // with log2(e)
 };
 
-__device__ inline void agent_store(float *p, float a, float b)
-{
-    union { float f[2]; uint64_t u; } w = {{a, b}};
-    __hip_atomic_store((uint64_t *)p, w.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ inline void agent_load(const float *p, float &a, float &b)
-{
-    union { uint64_t u; float f[2]; } w;
-    w.u = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    a = w.f[0]; b = w.f[1];
-}
-
 // maximum / sum over the 4 lanes that hold one query (lanes n, n + 16, n + 32, n + 48)
 __device__ inline float max4(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
 __device__ inline float sum4(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
 
-// [first token, end) that sequence b attends to, and the units that cover it (at least one, so that every output is written)
+// The tokens [lo, hi) that a sequence of length n attends to, and the units that cover them (at least one, so that
+// every output is written).
 struct Span { int lo, hi, unit0, units; };
-__device__ inline Span span_of(const AttnArgs &a, int b)
+__device__ inline Span span_of(const AttnArgs &a, int n)
 {
     Span s;
-    const int64_t room = (int64_t)a.width << a.page_log;
-    int n = a.lengths[b];
-    n = n < 0 ? 0 : n;
-    if (n > room) n = (int)room;
+    const int room = a.width << a.page_log;      // at most 2^30
+    n = n < 0 ? 0 : n > room ? room : n;
     s.hi = n;
     s.lo = a.window > 0 && n > a.window ? n - a.window : 0;
     s.unit0 = s.lo / kUnit;
     s.units = n > 0 ? (n - 1) / kUnit - s.unit0 + 1 : 1;
     return s;
 }
+
+// Walks the segments: 64 sequences at a time, one to a lane.
+struct Place {
+    int chunk, length;                           // the lanes' sequences 64 chunk + lane, and their lengths
+    int b;                                       // current sequence, the number of its first unit and its span
+    uint32_t base;
+    Span sp;
+    __device__ void lanes(const AttnArgs &a, int c, int lane)
+    {
+        chunk = c;
+        const int i = 64 * c + lane;
+        length = a.lengths[i < a.batch ? i : a.batch - 1];
+    }
+    __device__ void sequence(const AttnArgs &a, int i, int lane)
+    {
+        b = i;
+        if (i >> 6 != chunk) lanes(a, i >> 6, lane);
+        sp = span_of(a, __builtin_amdgcn_readlane(length, i & 63));
+    }
+    __device__ void next(const AttnArgs &a, int lane, uint32_t hc)
+    {
+        base += (uint32_t)sp.units * hc;
+        sequence(a, b + 1, lane);
+    }
+};
 
 // One wave's state over the units of one head.
 template <int D>
@@ -114,344 +137,529 @@ struct Operand {
     static constexpr int kRowWords = D / 16 * (FMT == 0 ? 2 : 1) / 4;     // dwords of a value row in a lane
 };
 
-// 16 tokens of keys: token lane % 16, units of channels lane / 16 + 4 s
+// What a wave holds of a unit between its requests and its products.
 template <int D, int FMT>
-__device__ inline void load_keys(U4 *k, const uint8_t *page, int page_log, int tok, int lane)
+struct Keys {
+    U4 k[2][Operand<D, FMT>::kKeyLoads];
+    uint32_t scale[2];
+};
+template <int D, int FMT>
+struct Values {
+    uint32_t v[8][Operand<D, FMT>::kRowWords];
+    uint32_t scale[2];
+};
+
+// One (page, head) of the cache as a buffer: a request past `bytes` returns 0 and costs nothing, which keeps the requests of a
+// loop unconditional and their number in flight known.
+__device__ inline __amdgpu_buffer_rsrc_t attn_rsrc(const void *p, uint32_t bytes)
 {
-#pragma unroll
-    for (int s = 0; s < Operand<D, FMT>::kKeyLoads; ++s)
-        k[s] = *(const U4 *)(page + ((((s * 4 + (lane >> 4)) << page_log) + tok + (lane & 15)) << 4));
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, kRsrcRaw);
 }
-// 4 rows of values, tokens 4 (lane / 16) + i, channels (lane % 16) * D/16 ...
+
+struct Head {                                    // of the segment at hand
+    int64_t page_bytes, at;                      // of a page, of this head in it
+    uint32_t bytes;                              // of this head in a page
+    int page_log, head, kv_heads;
+};
+
+// keys of 2 x 16 tokens: token lane % 16, units of channels lane / 16 + 4 s; pages pg[0], pg[1] (negative: none)
 template <int D, int FMT>
-__device__ inline void load_values(uint32_t *v, const uint8_t *page, int tok, int lane)
+__device__ inline void load_keys(Keys<D, FMT> &x, const AttnArgs &a, const Head &h, const int (&pg)[2], int t0, bool on, int lane)
 {
-    constexpr int W = Operand<D, FMT>::kRowWords;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint8_t *p = page + (tok + 4 * (lane >> 4) + i) * (D * (FMT == 0 ? 2 : 1)) + (lane & 15) * (4 * W);
-        if constexpr (W % 4 == 0)
+    for (int i = 0; i < 2; ++i) {
+        const int64_t p = pg[i] < 0 ? 0 : pg[i];
+        const int tok = (t0 + 16 * i) & ((1 << h.page_log) - 1);
+        const __amdgpu_buffer_rsrc_t r = attn_rsrc(a.k + p * h.page_bytes + h.at, on ? h.bytes : 0);
 #pragma unroll
-            for (int x = 0; x < W; x += 4) { const U4 y = *(const U4 *)(p + 4 * x); v[i * W + x] = y[0]; v[i * W + x + 1] = y[1]; v[i * W + x + 2] = y[2]; v[i * W + x + 3] = y[3]; }
-        else if constexpr (W == 2) { const uint2 y = *(const uint2 *)p; v[i * W] = y.x; v[i * W + 1] = y.y; }
-        else v[i * W] = *(const uint32_t *)p;
+        for (int s = 0; s < Operand<D, FMT>::kKeyLoads; ++s)
+            x.k[i][s] = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(r, (((s * 4 + (lane >> 4)) << h.page_log) + (lane & 15)) << 4, tok << 4, kOnce));
+        if constexpr (FMT == 1) {
+            const __amdgpu_buffer_rsrc_t q = attn_rsrc(a.ks + ((p * h.kv_heads + h.head) << h.page_log), on ? 1 << h.page_log : 0);
+            x.scale[i] = __builtin_amdgcn_raw_buffer_load_b32(q, 4 * (lane >> 4), tok, kOnce);
+        }
+    }
+}
+// rows of values: tokens 16 i + 4 (lane / 16) + j, channels (lane % 16) * D/16 ...
+template <int D, int FMT>
+__device__ inline void load_values(Values<D, FMT> &x, const AttnArgs &a, const Head &h, const int (&pg)[2], int t0, int lane)
+{
+    constexpr int W = Operand<D, FMT>::kRowWords, kRowBytes = D * (FMT == 0 ? 2 : 1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t p = pg[i] < 0 ? 0 : pg[i];
+        const int tok = (t0 + 16 * i) & ((1 << h.page_log) - 1);
+        const __amdgpu_buffer_rsrc_t r = attn_rsrc(a.v + p * h.page_bytes + h.at, h.bytes);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int off = (4 * (lane >> 4) + j) * kRowBytes + (lane & 15) * (4 * W);
+            uint32_t *v = x.v[4 * i + j];
+            if constexpr (W % 4 == 0)
+#pragma unroll
+                for (int w = 0; w < W; w += 4) {
+                    const U4 y = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 4 * w, tok * kRowBytes, kOnce));
+                    v[w] = y[0]; v[w + 1] = y[1]; v[w + 2] = y[2]; v[w + 3] = y[3];
+                }
+            else if constexpr (W == 2) {
+                const U2 y = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, off, tok * kRowBytes, kOnce));
+                v[0] = y[0]; v[1] = y[1];
+            } else
+                v[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, tok * kRowBytes, kOnce);
+        }
+        if constexpr (FMT == 1) {
+            const __amdgpu_buffer_rsrc_t q = attn_rsrc(a.vs + ((p * h.kv_heads + h.head) << h.page_log), 1 << h.page_log);
+            x.scale[i] = __builtin_amdgcn_raw_buffer_load_b32(q, 4 * (lane >> 4), tok, kOnce);
+        }
     }
 }
 
+// log2-scaled scores of a unit: x[8], token 16 (j / 4) + 4 (lane / 16) + j % 4, query lane % 16
 template <int D, int FMT>
-__global__ __launch_bounds__(64 * kAttnWaves, D == 256 ? 1 : 2) void paged_attention_kernel(const AttnArgs a)
+__device__ inline void scores(float (&x)[8], const Keys<D, FMT> &k, const half8v (&q)[D / 32], float scale)
 {
-    using Op = Operand<D, FMT>;
-    constexpr int R = D / 16, KL = Op::kKeyLoads, VW = Op::kRowWords, EB = FMT == 0 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        F4 s4 = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < Operand<D, FMT>::kKeyLoads; ++s) {
+            if constexpr (FMT == 0) {
+                s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, k.k[i][s]), q[s], s4, 0, 0, 0);
+            } else {
+                s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e4m3(k.k[i][s][0], k.k[i][s][1], 1.0f), q[2 * s], s4, 0, 0, 0);
+                s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e4m3(k.k[i][s][2], k.k[i][s][3], 1.0f), q[2 * s + 1], s4, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[4 * i + j] = s4[j] * scale;
+            if constexpr (FMT == 1) x[4 * i + j] *= __uint_as_float(((k.scale[i] >> (8 * j)) & 255) << 23);
+        }
+    }
+}
+
+// The unit's tokens outside [lo, hi) or on pages that are not there: scores -inf, and values 0 (such places may hold NaN).
+template <int D, int FMT>
+__device__ inline void mask(float (&x)[8], Values<D, FMT> &v, const int (&pg)[2], int t0, int lo, int hi, int lane)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int t = t0 + 16 * (j >> 2) + 4 * (lane >> 4) + (j & 3);
+        const bool in = t >= lo && t < hi && pg[j >> 2] >= 0;
+        x[j] = in ? x[j] : -INFINITY;
+#pragma unroll
+        for (int w = 0; w < Operand<D, FMT>::kRowWords; ++w) v.v[j][w] = in ? v.v[j][w] : 0u;
+        if constexpr (FMT == 1) if (!in) v.scale[j >> 2] = (v.scale[j >> 2] & ~(255u << (8 * (j & 3)))) | (127u << (8 * (j & 3)));
+    }
+}
+
+// The running maximum, sum and result take in a unit.
+template <int D, int FMT>
+__device__ inline void take_in(Running<D> &st, const float (&x)[8], const Values<D, FMT> &v)
+{
+    constexpr int R = D / 16;
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    top = fmaxf(st.m, max4(top));
+    if (__ballot(top > st.m)) {
+        const float f = top > st.m ? __builtin_amdgcn_exp2f(st.m - top) : 1.0f;
+        st.l *= f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) st.acc[r] *= f;
+        st.m = top;
+    }
+    const float off = (st.m == -INFINITY ? 0.0f : st.m) - kPShift;
+    half8v p, rest;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float e = __builtin_amdgcn_exp2f(x[j] - off);
+        st.l += e;
+        p[j] = (_Float16)e;
+        rest[j] = (_Float16)(e - (float)p[j]);
+    }
+    // O^T += V^T P^T, one tile of 16 channels after the other
+    if constexpr (FMT == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            U4 f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) f[y] = __builtin_amdgcn_perm(v.v[2 * y + 1][r / 2], v.v[2 * y][r / 2], r & 1 ? 0x07060302u : 0x05040100u);
+            st.acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, f), p, st.acc[r], 0, 0, 0);
+            st.acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, f), rest, st.acc[r], 0, 0, 0);
+        }
+    } else {
+        float vs[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vs[j] = __uint_as_float(((v.scale[j >> 2] >> (8 * (j & 3))) & 255) << 23);
+#pragma unroll
+        for (int r = 0; r < R; r += 2) {
+            uint32_t c[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[j] = f16x2_of_e4m3(v.v[j][r / 4], vs[j], (r / 2) & 1);
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                U4 f;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) f[y] = __builtin_amdgcn_perm(c[2 * y + 1], c[2 * y], z ? 0x07060302u : 0x05040100u);
+                st.acc[r + z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, f), p, st.acc[r + z], 0, 0, 0);
+                st.acc[r + z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, f), rest, st.acc[r + z], 0, 0, 0);
+            }
+        }
+    }
+}
+
+__device__ inline float lse_of(float m, float sum) { return sum == 0.0f ? -INFINITY : (m - kPShift + __builtin_amdgcn_logf(sum)) * kLn2; }
+
+// A segment that a wave has a share of, and where its results go.
+struct Segment {
+    int on, b, seg;
+    uint32_t seg0, seg1;
+};
+struct Target {
+    int queries;
+    int64_t o, lse;
+    __device__ Target(const AttnArgs &a, int b, int seg, int D)
+    {
+        const int head = seg / a.chunks, q0 = (seg - head * a.chunks) * kQueries;
+        queries = a.group - q0 < kQueries ? a.group - q0 : kQueries;
+        o = (int64_t)b * a.ldo + (int64_t)(head * a.group + q0) * D;
+        lse = ((int64_t)b * a.kv_heads + head) * a.group + q0;
+    }
+};
+
+// 8 channels of one query, with the maximum and sum that belong to them
+struct Eight {
+    float m, l, v[8];
+    __device__ void clear()
+    {
+        m = -INFINITY; l = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0;
+    }
+    __device__ void add(float pm, float pl, const F4 &lo, const F4 &hi)
+    {
+        const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.0f : top;
+        const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(pm - ref);
+        l = l * f + pl * g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = v[e] * f + (e < 4 ? lo[e & 3] : hi[e & 3]) * g;
+        m = top;
+    }
+    __device__ void result(const AttnArgs &a, const Target &to, int D, int query, int channel) const
+    {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        half8v h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = (_Float16)(v[e] * inv);
+        *(half8v *)(a.o + to.o + (int64_t)query * D + channel) = h;
+        if (a.lse && channel == 0) a.lse[to.lse + query] = lse_of(m, l);
+    }
+};
+
+template <int D> constexpr int part_floats() { return kQueries * (D + 4); }
+// Eight of the partial result in slot `slot`, through memory that all XCDs see
+template <int D>
+__device__ inline void store_part(__amdgpu_buffer_rsrc_t r, uint32_t slot, int query, int channel, const Eight &x)
+{
+    const uint32_t row = (slot * part_floats<D>() + query * (D + 4)) * 4u;
+    typedef decltype(__builtin_amdgcn_raw_buffer_load_b128(r, 0, 0, 0)) B4;
+    typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(r, 0, 0, 0)) B2;
+    if (channel == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B2, U2{__float_as_uint(x.m), __float_as_uint(x.l)}), r, row, 0, kAgent);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{x.v[0], x.v[1], x.v[2], x.v[3]}), r, row + (4 + channel) * 4u, 0, kAgent);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{x.v[4], x.v[5], x.v[6], x.v[7]}), r, row + (8 + channel) * 4u, 0, kAgent);
+}
+
+// Joins the partial results of blocks first, first + step, ... last of a segment, by the whole block: thread tid < items gets
+// the Eight of item0 + tid.  s: LDS of 10 floats per thread.
+template <int D, int THREADS>
+__device__ inline Eight join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Segment &g, uint32_t share, uint32_t first, uint32_t step, uint32_t last,
+                                   int item0, int items, int tid)
+{
+    // `lots` groups of threads take every lots-th part
+    const int lots = THREADS / items, lot = tid / items, i = item0 + tid - lot * items, query = i / (D / 8), channel = (i % (D / 8)) * 8;
+    constexpr int kBatch = 4;
+    Eight x;
+    x.clear();
+    if (lot < lots)
+        for (uint32_t j = first + lot * step; j <= last; j += kBatch * lots * step) {
+            F4 lo[kBatch], hi[kBatch];
+            U2 ml[kBatch];
+#pragma unroll
+            for (int z = 0; z < kBatch; ++z) {
+                const uint32_t k = j + z * lots * step;
+                // past the last one: a request beyond the buffer
+                const uint32_t row = k <= last ? ((2 * k + (g.seg0 >= k * share)) * part_floats<D>() + query * (D + 4)) * 4u : 0x80000000u;
+                ml[z] = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, row, 0, kAgent));
+                lo[z] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
+                hi[z] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (8 + channel) * 4u, 0, kAgent));
+            }
+#pragma unroll
+            for (int z = 0; z < kBatch; ++z)
+                if (j + z * lots * step <= last) x.add(__uint_as_float(ml[z][0]), __uint_as_float(ml[z][1]), lo[z], hi[z]);
+        }
+    if (lots > 1) {
+        F4 *sv = (F4 *)s;
+        float *sm = s + 8 * THREADS, *sl = sm + THREADS;
+        sv[2 * tid] = F4{x.v[0], x.v[1], x.v[2], x.v[3]};
+        sv[2 * tid + 1] = F4{x.v[4], x.v[5], x.v[6], x.v[7]};
+        sm[tid] = x.m;
+        sl[tid] = x.l;
+        __syncthreads();
+        if (tid < items) {
+            const int used = (int)((last - first) / step) + 1 < lots ? (int)((last - first) / step) + 1 : lots;
+            for (int k = 1; k < used; ++k) x.add(sm[tid + k * items], sl[tid + k * items], sv[2 * (tid + k * items)], sv[2 * (tid + k * items) + 1]);
+        }
+    }
+    __syncthreads();                             // all parts are read, and LDS is free again
+    return x;
+}
+
+// Counts an arrival; whether it was the last of `all`, after which the counter is 0 again.
+__device__ inline bool arrives_last(uint32_t *counter, uint32_t all)
+{
+    const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before != all - 1) return false;
+    __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+// What this wave stored is where all XCDs see it.
+__device__ inline void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <int D, int FMT>
+__global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kernel(const AttnArgs a)
+{
+    constexpr int WAVES = attn_waves<D>(), THREADS = 64 * WAVES, R = D / 16, EB = FMT == 0 ? 2 : 1;
     constexpr int kRow = D + 4;                  // floats of a row in LDS: rows of 16 queries fall on distinct banks
-    constexpr int kPart = kQueries * (D + 2);    // floats of a partial result
-    __shared__ __attribute__((aligned(16))) float s_o[kAttnWaves * kQueries * kRow];
-    __shared__ float s_m[256], s_l[256];
-    __shared__ int s_last;
+    extern __shared__ __attribute__((aligned(16))) float s_o[];          // [wave][2][rows][kRow], later the joins'
+    __shared__ float s_m[WAVES * 2 * kQueries], s_l[WAVES * 2 * kQueries];
+    __shared__ Segment s_seg[WAVES][2], s_out[2];
+    __shared__ int s_last[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int hc = a.kv_heads * a.chunks;
+    const uint32_t hc = (uint32_t)(a.kv_heads * a.chunks);
+    const int rows = a.group < kQueries ? a.group : kQueries;            // of a slot in LDS
 
-    // this block's place: lane i sums the units of `per` consecutive sequences
-    const int per = (a.batch + 63) / 64;
-    uint32_t mine = 0;
-    for (int j = 0; j < per; ++j) {
-        const int b = lane * per + j;
-        if (b < a.batch) mine += (uint32_t)span_of(a, b).units;
+    // the units of all sequences, 64 sequences at a time
+    uint32_t total = 0;
+#pragma unroll 4
+    for (int c = 0; c < (a.batch + 63) / 64; ++c) {
+        const int i = c * 64 + lane;
+        const int n = a.lengths[i < a.batch ? i : a.batch - 1];
+        total += i < a.batch ? (uint32_t)span_of(a, n).units : 0u;
     }
-    uint32_t upto = mine;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t x = __shfl_up(upto, d);
-        if (lane >= d) upto += x;
-    }
-    const uint32_t total = __shfl(upto, 63) * (uint32_t)hc;
-    uint32_t share = (total + gridDim.x - 1) / gridDim.x;
-    share = (share + kAttnWaves - 1) / kAttnWaves * kAttnWaves;
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+    total = (uint32_t)__builtin_amdgcn_readfirstlane((int)total) * hc;
+    const uint32_t mine = (total + gridDim.x * WAVES - 1) / (gridDim.x * WAVES), share = mine * WAVES;
     const uint32_t begin = blockIdx.x * share;
     if (begin >= total) return;
     const uint32_t end = begin + share < total ? begin + share : total;
+    const uint32_t wbegin = begin + wave * mine, wend = wbegin + mine < end ? wbegin + mine : end;
 
-    // the sequence that `begin` lies in, and the number of its first unit
-    const uint64_t before = __ballot(upto * (uint32_t)hc <= begin);
-    const int l0 = __popcll(before);             // lanes whose sequences all lie before
-    int b = l0 * per;
-    uint32_t base = l0 ? __shfl(upto, l0 - 1) * (uint32_t)hc : 0;
-    Span sp = span_of(a, b);
-    while (base + (uint32_t)sp.units * hc <= begin) { base += (uint32_t)sp.units * hc; ++b; sp = span_of(a, b); }
-
-    const int64_t head_bytes = (int64_t)D * EB << a.page_log, page_bytes = head_bytes * a.kv_heads;
     const int n = lane & 15, quarter = lane >> 4;
-
-    uint32_t at = begin;
-    while (at < end) {
-        while (base + (uint32_t)sp.units * hc <= at) { base += (uint32_t)sp.units * hc; ++b; sp = span_of(a, b); }
-        const int seg = (int)((at - base) / (uint32_t)sp.units);                  // which (head, chunk) of the sequence
-        const uint32_t seg0 = base + (uint32_t)seg * sp.units, seg1 = seg0 + sp.units;
-        const int head = seg / a.chunks, q0 = (seg - head * a.chunks) * kQueries;
-        const int queries = a.group - q0 < kQueries ? a.group - q0 : kQueries;
-        const uint32_t stop = seg1 < end ? seg1 : end;
-        const int u0 = sp.unit0 + (int)(at - seg0), u1 = sp.unit0 + (int)(stop - seg0);
-
-        Running<D> st;
-        st.clear();
-        half8v qf[D / 32];
-        {
-            const _Float16 *q = a.q + (int64_t)b * a.ldq + (int64_t)(head * a.group + q0 + (n < queries ? n : 0)) * D;
+    if (lane < 2) s_seg[wave][lane].on = 0;
+    if (tid < 2) { s_last[tid] = 0; s_out[tid].on = 0; }
+    if (wbegin < wend) {
+        Place pl;
+        pl.base = 0;
+        for (int c = 0;; ++c) {                  // the sequence that holds unit wbegin
+            pl.lanes(a, c, lane);
+            uint32_t upto = 64 * c + lane < a.batch ? (uint32_t)span_of(a, pl.length).units : 0u;
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
-                const int c = FMT == 0 ? s * 32 + quarter * 8 : ((s >> 1) * 4 + quarter) * 16 + (s & 1) * 8;
-                qf[s] = *(const half8v *)(q + c);
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
             }
+            const int before = __popcll(__ballot(pl.base + upto * hc <= wbegin));
+            if (before < 64) {
+                if (before) pl.base += (uint32_t)__builtin_amdgcn_readlane((int)upto, before - 1) * hc;
+                pl.sequence(a, 64 * c + before, lane);
+                break;
+            }
+            pl.base += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
         }
-        const int32_t *row = a.table + (int64_t)b * a.ld_table;
-        int pages = 0;
-        for (int u = u0 + wave, it = 0; u < u1 && sp.hi > 0; u += kAttnWaves, ++it) {
-            if ((it & 31) == 0) {                // the pages of this wave's next 32 units, two halves to a unit
-                int t = (u + (lane >> 1) * kAttnWaves) * kUnit + (lane & 1) * 16;
-                t = t < sp.hi ? t : sp.hi - 1;
-                pages = row[t >> a.page_log];
-                if ((uint32_t)pages >= (uint32_t)a.n_pages) pages = -1;
-            }
-            const int t0 = u * kUnit, mask = (1 << a.page_log) - 1;
-            int pg[2];
-            const uint8_t *vp[2];
-            U4 kf[2][KL];
-            uint32_t vr[8][VW];
-            uint32_t ksc[2], vsc[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                pg[h] = __builtin_amdgcn_readlane(pages, 2 * (it & 31) + h);
-                const int64_t p = pg[h] < 0 ? 0 : pg[h];
-                const int tok = (t0 + 16 * h) & mask;
-                load_keys<D, FMT>(kf[h], a.k + p * page_bytes + head * head_bytes, a.page_log, tok, lane);
-                vp[h] = a.v + p * page_bytes + head * head_bytes;
-                if constexpr (FMT == 1) {
-                    const int64_t so = ((p * a.kv_heads + head) << a.page_log) + tok + 4 * quarter;
-                    ksc[h] = *(const uint32_t *)(a.ks + so);
-                    vsc[h] = *(const uint32_t *)(a.vs + so);
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) load_values<D, FMT>(vr[4 * h], vp[h], (t0 + 16 * h) & mask, lane);
+        Head h;
+        h.page_log = a.page_log;
+        h.kv_heads = a.kv_heads;
+        h.bytes = (uint32_t)(D * EB) << a.page_log;
+        h.page_bytes = (int64_t)h.bytes * a.kv_heads;
 
-            float x[2][4];
+        uint32_t at = wbegin;
+        while (at < wend) {
+            while (pl.base + (uint32_t)pl.sp.units * hc <= at) pl.next(a, lane, hc);
+            const int seg = (int)((at - pl.base) / (uint32_t)pl.sp.units);
+            const uint32_t seg0 = pl.base + (uint32_t)seg * pl.sp.units, seg1 = seg0 + pl.sp.units;
+            const uint32_t stop = seg1 < wend ? seg1 : wend;
+            const int u0 = pl.sp.unit0 + (int)(at - seg0), u1 = pl.sp.unit0 + (int)(stop - seg0), lo = pl.sp.lo, hi = pl.sp.hi;
+            const Target to(a, pl.b, seg, D);
+            h.head = seg / a.chunks;
+            h.at = (int64_t)h.bytes * h.head;
+
+            Running<D> st;
+            st.clear();
+            if (hi > 0) {
+                const int32_t *row = a.table + (int64_t)pl.b * a.ld_table;
+                int pages = 0;
+                // the pages of the next 32 units, two halves to a unit
+                const auto turn = [&](int u) {
+                    int t = (u + (lane >> 1)) * kUnit + (lane & 1) * 16;
+                    t = t < hi ? t : hi - 1;
+                    pages = row[t >> a.page_log];
+                    if ((uint32_t)pages >= (uint32_t)a.n_pages) pages = -1;
+                };
+                const auto page_of = [&](int (&pg)[2], int i) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                F4 s4 = {0, 0, 0, 0};
+                    for (int z = 0; z < 2; ++z) pg[z] = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + z);
+                };
+                half8v q[D / 32];
+                const _Float16 *qp = a.q + (int64_t)pl.b * a.ldq + (to.o - (int64_t)pl.b * a.ldo) + (int64_t)(n < to.queries ? n : 0) * D;
 #pragma unroll
-                for (int s = 0; s < KL; ++s) {
-                    if constexpr (FMT == 0) {
-                        union { U4 u; half8v h8; } c = {kf[h][s]};
-                        s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(c.h8, qf[s], s4, 0, 0, 0);
-                    } else {
-                        s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e4m3(kf[h][s][0], kf[h][s][1], 1.0f), qf[2 * s], s4, 0, 0, 0);
-                        s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e4m3(kf[h][s][2], kf[h][s][3], 1.0f), qf[2 * s + 1], s4, 0, 0, 0);
+                for (int s = 0; s < D / 32; ++s)
+                    q[s] = *(const half8v *)(qp + (FMT == 0 ? s * 32 + quarter * 8 : ((s >> 1) * 4 + quarter) * 16 + (s & 1) * 8));
+                turn(u0);
+                int pg[2];
+                page_of(pg, 0);
+                Keys<D, FMT> k;
+                load_keys<D, FMT>(k, a, h, pg, u0 * kUnit, true, lane);
+                for (int u = u0; u < u1; ++u) {
+                    Values<D, FMT> v;
+                    load_values<D, FMT>(v, a, h, pg, u * kUnit, lane);
+                    float x[8];
+                    scores<D, FMT>(x, k, q, a.scale);
+                    const int now[2] = {pg[0], pg[1]};
+                    // the next unit's keys are on their way through this one's softmax and values
+                    if (((u + 1 - u0) & 31) == 0) turn(u + 1);
+                    page_of(pg, u + 1 - u0);
+                    load_keys<D, FMT>(k, a, h, pg, (u + 1) * kUnit, u + 1 < u1, lane);
+                    if (u * kUnit < lo || (u + 1) * kUnit > hi || now[0] < 0 || now[1] < 0) mask<D, FMT>(x, v, now, u * kUnit, lo, hi, lane);
+                    take_in<D, FMT>(st, x, v);
+                }
+            }
+            const float l = sum4(st.l);
+            if (at == seg0 && stop == seg1) {    // all of the segment is here
+                if (n < to.queries) {
+                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                    _Float16 *o = a.o + to.o + (int64_t)n * D + quarter * 4 * R;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (R == 4) {
+                            half4v y = {(_Float16)(st.acc[0][i] * inv), (_Float16)(st.acc[1][i] * inv), (_Float16)(st.acc[2][i] * inv), (_Float16)(st.acc[3][i] * inv)};
+                            *(half4v *)(o + i * R) = y;
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < R; r += 8) {
+                                half8v y;
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) y[e] = (_Float16)(st.acc[r + e][i] * inv);
+                                *(half8v *)(o + i * R + r) = y;
+                            }
+                        }
                     }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[h][i] = s4[i] * a.scale;
-                    if constexpr (FMT == 1) x[h][i] *= __uint_as_float(((ksc[h] >> (8 * i)) & 255) << 23);
-                }
-            }
-            // a unit that is not all there: scores -inf, and values 0 (what such places hold may be NaN)
-            if (t0 < sp.lo || t0 + kUnit > sp.hi || pg[0] < 0 || pg[1] < 0) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int t = t0 + 16 * (j >> 2) + 4 * quarter + (j & 3);
-                    const bool in = t >= sp.lo && t < sp.hi && pg[j >> 2] >= 0;
-                    if (!in) x[j >> 2][j & 3] = -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) vr[j][w] = in ? vr[j][w] : 0u;
-                    if constexpr (FMT == 1) if (!in) vsc[j >> 2] = (vsc[j >> 2] & ~(255u << (8 * (j & 3)))) | (127u << (8 * (j & 3)));
-                }
-            }
-            float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-            top = fmaxf(st.m, max4(top));
-            if (__ballot(top > st.m)) {
-                const float f = top > st.m ? __builtin_amdgcn_exp2f(st.m - top) : 1.0f;
-                st.l *= f;
-#pragma unroll
-                for (int r = 0; r < R; ++r) st.acc[r] *= f;
-                st.m = top;
-            }
-            const float off = (st.m == -INFINITY ? 0.0f : st.m) - kPShift;
-            half8v p, rest;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float e = __builtin_amdgcn_exp2f(x[j >> 2][j & 3] - off);
-                st.l += e;
-                p[j] = (_Float16)e;
-                rest[j] = (_Float16)(e - (float)p[j]);
-            }
-            // O^T += V^T P^T, one tile of 16 channels after the other
-            if constexpr (FMT == 0) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    union { half8v h; uint32_t u[4]; } f;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) f.u[y] = __builtin_amdgcn_perm(vr[2 * y + 1][r / 2], vr[2 * y][r / 2], r & 1 ? 0x07060302u : 0x05040100u);
-                    st.acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h, p, st.acc[r], 0, 0, 0);
-                    st.acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h, rest, st.acc[r], 0, 0, 0);
+                    if (a.lse && quarter == 0) a.lse[to.lse + n] = lse_of(st.m, l);
                 }
             } else {
-                float vs[8];
+                const int slot = 2 * wave + (seg0 >= wbegin);            // the segment that goes on from before, or the one that goes on after
+                if (lane == 0) s_seg[wave][seg0 >= wbegin] = {1, pl.b, seg, seg0, seg1};
+                if (quarter == 0) { s_m[slot * kQueries + n] = st.m; s_l[slot * kQueries + n] = l; }
+                if (n < to.queries) {
+                    float *o = s_o + (slot * rows + n) * kRow + quarter * 4 * R;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) vs[j] = __uint_as_float(((vsc[j >> 2] >> (8 * (j & 3))) & 255) << 23);
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < R; r += 2) {
-                    uint32_t c[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) c[j] = f16x2_of_e4m3(vr[j][r / 4], vs[j], (r / 2) & 1);
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        union { half8v h; uint32_t u[4]; } f;
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) f.u[y] = __builtin_amdgcn_perm(c[2 * y + 1], c[2 * y], z ? 0x07060302u : 0x05040100u);
-                        st.acc[r + z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h, p, st.acc[r + z], 0, 0, 0);
-                        st.acc[r + z] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h, rest, st.acc[r + z], 0, 0, 0);
-                    }
+                        for (int r = 0; r < R; r += 4) *(F4 *)(o + i * R + r) = F4{st.acc[r][i], st.acc[r + 1][i], st.acc[r + 2][i], st.acc[r + 3][i]};
                 }
             }
+            at = stop;
         }
+    }
+    __syncthreads();
 
-        // the waves' results side by side in LDS
-        const float l = sum4(st.l);
-        if (quarter == 0) { s_m[wave * kQueries + n] = st.m; s_l[wave * kQueries + n] = l; }
-        if (n < queries) {
-            float *o = s_o + (wave * kQueries + n) * kRow;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < R; r += 4)
-                    *(F4 *)(o + (quarter * 4 + i) * R + r) = F4{st.acc[r][i], st.acc[r + 1][i], st.acc[r + 2][i], st.acc[r + 3][i]};
-        }
-        __syncthreads();
-        const bool whole = at == seg0 && stop == seg1;
-        const int items = queries * (D / 8);     // 8 channels of one query each
-        const int64_t out_row = (int64_t)b * a.ldo + (int64_t)(head * a.group + q0) * D;
-        const int64_t lse_row = (int64_t)b * a.kv_heads * a.group + head * a.group + q0;
-        float *part = a.partial + (size_t)(2 * blockIdx.x + (seg0 >= begin)) * kPart;
-        for (int i = tid; i < items; i += 64 * kAttnWaves) {
-            const int qi = i / (D / 8), c = (i % (D / 8)) * 8;
-            float m = s_m[qi], sum = 0, v[8] = {};
-#pragma unroll
-            for (int w = 1; w < kAttnWaves; ++w) m = fmaxf(m, s_m[w * kQueries + qi]);
-            const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int w = 0; w < kAttnWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(s_m[w * kQueries + qi] - ref);
-                sum += f * s_l[w * kQueries + qi];
-                const float *o = s_o + (w * kQueries + qi) * kRow + c;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += f * o[e];
+    // segments that began with a wave's last units (or before the block) and go on: joined by that wave over the waves behind
+    const __amdgpu_buffer_rsrc_t parts = attn_rsrc(a.partial, 2 * kAttnBlocks * part_floats<D>() * 4);
+    for (int z = wave == 0 ? 0 : 1; z < 2; ++z) {
+        const Segment g = s_seg[wave][z];
+        if (!g.on) continue;
+        int wl = wave;
+        while (wl + 1 < WAVES && s_seg[wl + 1][0].on && s_seg[wl + 1][0].seg0 == g.seg0) ++wl;
+        const Target to(a, g.b, g.seg, D);
+        const bool whole = g.seg0 >= begin && g.seg1 <= end;
+        for (int i = lane; i < to.queries * (D / 8); i += 64) {
+            const int query = i / (D / 8), channel = (i % (D / 8)) * 8;
+            Eight x;
+            x.clear();
+            for (int w = wave; w <= wl; ++w) {
+                const int slot = 2 * w + (w == wave ? z : 0);
+                const float *o = s_o + (slot * rows + query) * kRow + channel;
+                x.add(s_m[slot * kQueries + query], s_l[slot * kQueries + query], *(const F4 *)o, *(const F4 *)(o + 4));
             }
-            if (whole) {
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                half8v h;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = (_Float16)(v[e] * inv);
-                *(half8v *)(a.o + out_row + (int64_t)qi * D + c) = h;
-                if (a.lse && c == 0) a.lse[lse_row + qi] = sum == 0.0f ? -INFINITY : (m - kPShift + __builtin_amdgcn_logf(sum)) * kLn2;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) agent_store(part + 2 * kQueries + qi * D + c + e, v[e], v[e + 1]);
-                if (c == 0) agent_store(part + 2 * qi, m, sum);
-            }
+            if (whole) x.result(a, to, D, query, channel);
+            else store_part<D>(parts, 2 * blockIdx.x + (g.seg0 >= begin), query, channel, x);
         }
         if (!whole) {
-            // every store of this block is at the agent's point of coherence before its arrival is counted
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            const uint32_t first = seg0 / share, last = (seg1 - 1) / share;        // blocks that share this head
-            if (tid == 0) {
-                uint32_t *arrived = a.arrived + (size_t)b * hc + seg;
-                const uint32_t before_me = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = before_me == last - first;
-                if (before_me == last - first) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            if (s_last) {
-                // `lots` groups of threads each take every lots-th part; a thread has 8 channels of one query
-                const int lots = items < 256 ? 256 / items : 1;
-                const int lot = tid / items;
-                for (int i = lots > 1 ? tid - lot * items : tid; i < items && lot < (lots > 1 ? lots : 1 << 30); i += lots > 1 ? items : 256) {
-                    const int qi = i / (D / 8), c = (i % (D / 8)) * 8;
-                    float m = -INFINITY, sum = 0, v[8] = {};
-                    constexpr int kBatch = 4;
-                    const int my = lots > 1 ? lot : 0;
-                    for (uint32_t j = first + my; j <= last; j += (uint32_t)(kBatch * lots)) {
-                        float pm[kBatch], pl[kBatch], pv[kBatch][8];
-#pragma unroll
-                        for (int z = 0; z < kBatch; ++z) {
-                            const uint32_t jj = j + z * lots <= last ? j + z * lots : j;
-                            const float *pp = a.partial + (size_t)(2 * jj + (seg0 >= jj * share)) * kPart;
-                            agent_load(pp + 2 * qi, pm[z], pl[z]);
-#pragma unroll
-                            for (int e = 0; e < 8; e += 2) agent_load(pp + 2 * kQueries + qi * D + c + e, pv[z][e], pv[z][e + 1]);
-                        }
-#pragma unroll
-                        for (int z = 0; z < kBatch; ++z)
-                            if (j + z * lots <= last) {
-                                const float top = fmaxf(m, pm[z]), ref = top == -INFINITY ? 0.0f : top;
-                                const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(pm[z] - ref);
-                                sum = sum * f + pl[z] * g;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] = v[e] * f + pv[z][e] * g;
-                                m = top;
-                            }
-                    }
-                    if (lots > 1) {              // side by side in LDS again
-                        float *o = s_o + (lot * items + i) * 8;
-                        *(F4 *)o = F4{v[0], v[1], v[2], v[3]};
-                        *(F4 *)(o + 4) = F4{v[4], v[5], v[6], v[7]};
-                        s_m[lot * items + i] = m;
-                        s_l[lot * items + i] = sum;
-                    } else {
-                        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                        half8v h;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) h[e] = (_Float16)(v[e] * inv);
-                        *(half8v *)(a.o + out_row + (int64_t)qi * D + c) = h;
-                        if (a.lse && c == 0) a.lse[lse_row + qi] = sum == 0.0f ? -INFINITY : (m - kPShift + __builtin_amdgcn_logf(sum)) * kLn2;
-                    }
-                }
-                if (lots > 1) {
-                    __syncthreads();
-                    if (tid < items) {
-                        const int qi = tid / (D / 8), c = (tid % (D / 8)) * 8;
-                        float m = -INFINITY, sum = 0, v[8] = {};
-                        for (int g = 0; g < lots; ++g) m = fmaxf(m, s_m[g * items + tid]);
-                        const float ref = m == -INFINITY ? 0.0f : m;
-                        for (int g = 0; g < lots; ++g) {
-                            const float f = __builtin_amdgcn_exp2f(s_m[g * items + tid] - ref);
-                            sum += f * s_l[g * items + tid];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] += f * s_o[(g * items + tid) * 8 + e];
-                        }
-                        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                        half8v h;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) h[e] = (_Float16)(v[e] * inv);
-                        *(half8v *)(a.o + out_row + (int64_t)qi * D + c) = h;
-                        if (a.lse && c == 0) a.lse[lse_row + qi] = sum == 0.0f ? -INFINITY : (m - kPShift + __builtin_amdgcn_logf(sum)) * kLn2;
-                    }
-                }
+            stores_done();
+            if (lane == 0) {
+                const uint32_t first = g.seg0 / share, last = (g.seg1 - 1) / share, all = last - first + 1;
+                const uint32_t group = (blockIdx.x - first) / kGroupParts * kGroupParts + first;
+                const bool in_groups = all > kGroupParts;
+                uint32_t *counter = in_groups ? a.arrived + 2 * group + (g.seg0 >= group * share) : a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg;
+                const uint32_t of = in_groups ? (last - group + 1 < kGroupParts ? last - group + 1 : kGroupParts) : all;
+                s_last[g.seg0 >= begin] = arrives_last(counter, of);
+                s_out[g.seg0 >= begin] = g;
             }
         }
-        __syncthreads();                         // LDS is the next head's
-        at = stop;
+    }
+    __syncthreads();
+
+    // the segments shared with other blocks whose last share has now arrived
+    for (int z = 0; z < 2; ++z) {
+        if (!s_last[z]) continue;
+        const Segment g = s_out[z];
+        const Target to(a, g.b, g.seg, D);
+        const uint32_t first = g.seg0 / share, last = (g.seg1 - 1) / share;
+        const int items = to.queries * (D / 8);
+        const bool in_groups = last - first + 1 > kGroupParts;
+        bool final = !in_groups;
+        if (in_groups) {                         // the group's result takes the place of its first part
+            const uint32_t group = (blockIdx.x - first) / kGroupParts * kGroupParts + first;
+            const uint32_t of = group + kGroupParts - 1 < last ? group + kGroupParts - 1 : last;
+            for (int i0 = 0; i0 < items; i0 += THREADS) {
+                const int some = items - i0 < THREADS ? items - i0 : THREADS;
+                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, group, 1, of, i0, some, tid);
+                if (tid < some) store_part<D>(parts, 2 * group + (g.seg0 >= group * share), (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8, x);
+            }
+            stores_done();
+            __syncthreads();
+            if (tid == 0) s_last[z] = arrives_last(a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg, (last - first) / kGroupParts + 1);
+            __syncthreads();
+            final = s_last[z];
+        }
+        if (final)
+            for (int i0 = 0; i0 < items; i0 += THREADS) {
+                const int some = items - i0 < THREADS ? items - i0 : THREADS;
+                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, first, in_groups ? kGroupParts : 1, last, i0, some, tid);
+                if (tid < some) x.result(a, to, D, (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8);
+            }
     }
 }
 
 static int attn_chunks(const paro_kv_cache &c, int q_heads) { return (q_heads / c.kv_heads + kQueries - 1) / kQueries; }
-static size_t attn_part_bytes(const paro_kv_cache &c) { return sizeof(float) * kQueries * (c.head_dim + 2); }
+static size_t attn_part_bytes(const paro_kv_cache &c) { return sizeof(float) * kQueries * (c.head_dim + 4); }
 static size_t attn_scratch_bytes(const paro_kv_cache &c) { return ((size_t)2 * kAttnBlocks * attn_part_bytes(c) + 255) / 256 * 256; }
 
 template <int D, int FMT>
-static hipError_t launch_attention(const AttnArgs &a, int blocks, hipStream_t s)
+static hipError_t launch_attention(const AttnArgs &a, int64_t units, hipStream_t s)
 {
-    hipLaunchKernelGGL((paged_attention_kernel<D, FMT>), dim3(blocks), dim3(64 * kAttnWaves), 0, s, a);
+    constexpr int WAVES = attn_waves<D>();
+    // no more waves than the longest sequences could have units
+    const int64_t blocks = (units + WAVES - 1) / WAVES;
+    const int rows = a.group < kQueries ? a.group : kQueries;
+    const size_t shares = sizeof(float) * WAVES * 2 * rows * (D + 4), joins = sizeof(float) * 10 * 64 * WAVES;
+    static std::atomic<uint64_t> attr_done{0};
+    if (const int dev = once_pending(attr_done); dev >= 0) {
+        const hipError_t e = hipFuncSetAttribute((const void *)paged_attention_kernel<D, FMT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)(sizeof(float) * WAVES * 2 * kQueries * (D + 4)));
+        if (e != hipSuccess) return e;
+        once_done(attr_done, dev);
+    }
+    hipLaunchKernelGGL((paged_attention_kernel<D, FMT>), dim3((unsigned)(blocks < kAttnBlocks ? blocks : kAttnBlocks)), dim3(64 * WAVES),
+                       shares > joins ? shares : joins, s, a);
     return hipGetLastError();
 }
 
@@ -461,7 +669,7 @@ extern "C" size_t paro_workspace_exchange_bytes_attention(const paro_kv_cache *c
 {
     using namespace paro;
     if (!cache || cache->kv_heads <= 0 || q_heads <= 0 || q_heads % cache->kv_heads || batch <= 0) return 0;
-    const size_t counters = (size_t)batch * cache->kv_heads * attn_chunks(*cache, q_heads) * sizeof(uint32_t);
+    const size_t counters = (2 * kAttnBlocks + (size_t)batch * cache->kv_heads * attn_chunks(*cache, q_heads)) * sizeof(uint32_t);
     return kWsPartialOff + (counters + 255) / 256 * 256;
 }
 
@@ -503,20 +711,18 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     a.page_log = log2_of(c.page); a.n_pages = c.n_pages; a.kv_heads = c.kv_heads; a.group = q_heads / c.kv_heads;
     a.chunks = attn_chunks(c, q_heads); a.width = table_width; a.batch = batch; a.window = window;
     a.scale = scale * kLog2e;
-    // no more blocks than the longest sequences could fill with a unit for every wave
     int64_t seen = tokens;
     if (window > 0 && window + 2 * kUnit < seen) seen = window + 2 * kUnit;
     const int64_t most = units * ((seen + kUnit - 1) / kUnit);
-    const int blocks = (int)(most / kAttnWaves + 1 < kAttnBlocks ? most / kAttnWaves + 1 : kAttnBlocks);
     hipStream_t s = (hipStream_t)stream;
     hipError_t e;
     switch (c.head_dim * 2 + c.format) {
-    case 128: e = launch_attention<64, 0>(a, blocks, s); break;
-    case 129: e = launch_attention<64, 1>(a, blocks, s); break;
-    case 256: e = launch_attention<128, 0>(a, blocks, s); break;
-    case 257: e = launch_attention<128, 1>(a, blocks, s); break;
-    case 512: e = launch_attention<256, 0>(a, blocks, s); break;
-    default: e = launch_attention<256, 1>(a, blocks, s); break;
+    case 128: e = launch_attention<64, 0>(a, most, s); break;
+    case 129: e = launch_attention<64, 1>(a, most, s); break;
+    case 256: e = launch_attention<128, 0>(a, most, s); break;
+    case 257: e = launch_attention<128, 1>(a, most, s); break;
+    case 512: e = launch_attention<256, 0>(a, most, s); break;
+    default: e = launch_attention<256, 1>(a, most, s); break;
     }
     return e == hipSuccess ? PARO_OK : PARO_ERR_HIP;
 }

@@ -73,9 +73,9 @@ def test_attention_refusals_and_workspace():
     assert f(ws=None) == E_WS and f(n=need - 1) == E_WS
     assert f(width=1 << 27, ldt=1 << 27) == E_UNSUP and f(batch=1 << 20, width=1 << 14, ldt=0, n=1 << 40) == E_UNSUP
     ex = L.paro_workspace_exchange_bytes_attention(r(_cache()), 8, 3)
-    assert ex == 256 + 256 and need > ex
-    assert L.paro_workspace_exchange_bytes_attention(r(_cache()), 8, 1000) == 256 + 8192      # 2000 counters
-    assert L.paro_workspace_exchange_bytes_attention(r(_cache(kv_heads=1)), 40, 100) == 256 + 1280        # 3 x 16 query heads
+    assert ex == 256 + 2304 and need > ex                             # 512 counters of groups of blocks, 6 of heads
+    assert L.paro_workspace_exchange_bytes_attention(r(_cache()), 8, 1000) == 256 + 10240     # 2000 heads
+    assert L.paro_workspace_exchange_bytes_attention(r(_cache(kv_heads=1)), 40, 100) == 256 + 3328        # 3 x 16 query heads
     assert L.paro_workspace_bytes_attention(r(_cache()), 7, 3) == 0 and L.paro_workspace_bytes_attention(None, 8, 3) == 0
     assert L.paro_workspace_bytes_attention(r(_cache()), 8, 0) == 0
 
