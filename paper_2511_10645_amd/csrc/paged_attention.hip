@@ -30,7 +30,11 @@ namespace paro {
 constexpr int kUnit = 32;                        // tokens of a unit
 constexpr int kAttnBlocks = 256;                 // most blocks of a launch: one for every compute unit
 constexpr int kQueries = 16;                     // query heads of a unit: the N of the matrix instruction
-constexpr int kGroupParts = 32;                  // partial results that are joined at once
+#ifndef LEAST
+#define LEAST 4
+#endif
+constexpr uint32_t kLeastUnits = LEAST;              // of a block
+constexpr uint32_t kGroupParts = 32;                  // partial results that are joined at once
 constexpr float kPShift = 15.0f;                 // p is held 2^15 times
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRsrcRaw = 0x00020000;             // raw buffer, 32-bit data format
@@ -57,12 +61,36 @@ struct AttnArgs {
     float *partial;                              // [2 * kAttnBlocks][kQueries * (D + 4)]: m, l, then the row, of every query
     int64_t ldq, ldo, ld_table;
     int page_log, n_pages, kv_heads, group, chunks, width, batch, window;
+    float per_block;                             // 1 / blocks
     float scale;                                 // with log2(e)
 };
 
-// maximum / sum over the 4 lanes that hold one query (lanes n, n + 16, n + 32, n + 48)
-__device__ inline float max4(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
-__device__ inline float sum4(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
+// The other three of the 4 lanes that hold one query are lanes n ^ 16, n ^ 32, n ^ 48: two exchanges of rows of lanes.
+__device__ inline float max4(float x)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ inline float sum4(float x)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+// Sums over lanes 0..lane.
+__device__ inline uint32_t sums_upto(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);       // row_shr 1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);       // row_bcast 15 into rows 1 and 3
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);       // row_bcast 31 into rows 2 and 3
+    return x;
+}
 
 // The tokens [lo, hi) that a sequence of length n attends to, and the units that cover them (at least one, so that
 // every output is written).
@@ -308,20 +336,50 @@ __device__ inline void take_in(Running<D> &st, const float (&x)[8], const Values
 
 __device__ inline float lse_of(float m, float sum) { return sum == 0.0f ? -INFINITY : (m - kPShift + __builtin_amdgcn_logf(sum)) * kLn2; }
 
-// A segment that a wave has a share of, and where its results go.
+// x / d for a quotient up to 2^22, inv = 1 / d in fp32.
+__device__ inline uint32_t quotient(uint32_t x, uint32_t d, float inv)
+{
+    const uint32_t q = (uint32_t)((float)x * inv), r = x - q * d;        // off by one at most
+    return (int)r < 0 ? q - 1 : r >= d ? q + 1 : q;
+}
+
+// A segment that a wave has a share of: sequence, (head, chunk), its units.
 struct Segment {
-    int on, b, seg;
-    uint32_t seg0, seg1;
+    int b, seg;
+    uint32_t seg0, seg1;                         // seg1 0: none
+    __device__ Segment uniform() const           // as read from LDS, in scalar registers
+    {
+        return {__builtin_amdgcn_readfirstlane(b), __builtin_amdgcn_readfirstlane(seg), (uint32_t)__builtin_amdgcn_readfirstlane((int)seg0),
+                (uint32_t)__builtin_amdgcn_readfirstlane((int)seg1)};
+    }
 };
 struct Target {
-    int queries;
+    int head, first, queries;                    // key-value head, first query head, their number
     int64_t o, lse;
+    Target() = default;
     __device__ Target(const AttnArgs &a, int b, int seg, int D)
     {
-        const int head = seg / a.chunks, q0 = (seg - head * a.chunks) * kQueries;
-        queries = a.group - q0 < kQueries ? a.group - q0 : kQueries;
-        o = (int64_t)b * a.ldo + (int64_t)(head * a.group + q0) * D;
-        lse = ((int64_t)b * a.kv_heads + head) * a.group + q0;
+        int chunk = 0;
+        head = seg;
+        if (a.chunks > 1) { head = seg / a.chunks; chunk = seg - head * a.chunks; }
+        first = head * a.group + chunk * kQueries;
+        queries = a.group - chunk * kQueries < kQueries ? a.group - chunk * kQueries : kQueries;
+        o = (int64_t)b * a.ldo + (int64_t)first * D;
+        lse = (int64_t)b * (a.kv_heads * a.group) + first;
+    }
+};
+
+// The blocks that share a segment, and the group of them that block `me` is in.
+struct Sharers {
+    uint32_t first, last, group, group_last;
+    bool in_groups;
+    __device__ Sharers(const Segment &g, uint32_t share, float per_share, uint32_t me)
+    {
+        first = quotient(g.seg0, share, per_share);
+        last = quotient(g.seg1 - 1, share, per_share);
+        in_groups = last - first + 1 > kGroupParts;
+        group = (me - first) / kGroupParts * kGroupParts + first;
+        group_last = group + kGroupParts - 1 < last ? group + kGroupParts - 1 : last;
     }
 };
 
@@ -334,13 +392,29 @@ struct Eight {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 0;
     }
-    __device__ void add(float pm, float pl, const F4 &lo, const F4 &hi)
+    // Takes in those of N results that `which` has a bit for; all are read first.
+    template <int N, class Read>
+    __device__ void add(uint32_t which, Read read)
     {
-        const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.0f : top;
-        const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(pm - ref);
-        l = l * f + pl * g;
+        float pm[N], pl[N], top = m;
+        F4 lo[N], hi[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = v[e] * f + (e < 4 ? lo[e & 3] : hi[e & 3]) * g;
+        for (int k = 0; k < N; ++k) read(k, pm[k], pl[k], lo[k], hi[k]);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (which >> k & 1) top = fmaxf(top, pm[k]);
+        const float ref = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - ref);
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (which >> k & 1) {
+                const float g = __builtin_amdgcn_exp2f(pm[k] - ref);
+                l = fmaf(pl[k], g, l);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = fmaf(e < 4 ? lo[k][e & 3] : hi[k][e & 3], g, v[e]);
+            }
         m = top;
     }
     __device__ void result(const AttnArgs &a, const Target &to, int D, int query, int channel) const
@@ -374,26 +448,24 @@ __device__ inline Eight join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Seg
                                    int item0, int items, int tid)
 {
     // `lots` groups of threads take every lots-th part
-    const int lots = THREADS / items, lot = tid / items, i = item0 + tid - lot * items, query = i / (D / 8), channel = (i % (D / 8)) * 8;
-    constexpr int kBatch = 4;
+    constexpr int kLots = 8, kBatch = 4;
+    const int lots = THREADS / items < kLots ? THREADS / items : kLots;
+    const int lot = tid / items, i = item0 + tid - lot * items, query = i / (D / 8), channel = (i % (D / 8)) * 8;
     Eight x;
     x.clear();
     if (lot < lots)
         for (uint32_t j = first + lot * step; j <= last; j += kBatch * lots * step) {
-            F4 lo[kBatch], hi[kBatch];
-            U2 ml[kBatch];
-#pragma unroll
-            for (int z = 0; z < kBatch; ++z) {
+            const uint32_t left = (last - j) / (lots * step) + 1;
+            x.add<kBatch>((1u << (left < kBatch ? left : kBatch)) - 1, [&](int z, float &m, float &l, F4 &lo, F4 &hi) {
                 const uint32_t k = j + z * lots * step;
                 // past the last one: a request beyond the buffer
                 const uint32_t row = k <= last ? ((2 * k + (g.seg0 >= k * share)) * part_floats<D>() + query * (D + 4)) * 4u : 0x80000000u;
-                ml[z] = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, row, 0, kAgent));
-                lo[z] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
-                hi[z] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (8 + channel) * 4u, 0, kAgent));
-            }
-#pragma unroll
-            for (int z = 0; z < kBatch; ++z)
-                if (j + z * lots * step <= last) x.add(__uint_as_float(ml[z][0]), __uint_as_float(ml[z][1]), lo[z], hi[z]);
+                const U2 ml = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, row, 0, kAgent));
+                m = __uint_as_float(ml[0]);
+                l = __uint_as_float(ml[1]);
+                lo = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
+                hi = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (8 + channel) * 4u, 0, kAgent));
+            });
         }
     if (lots > 1) {
         F4 *sv = (F4 *)s;
@@ -404,8 +476,11 @@ __device__ inline Eight join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Seg
         sl[tid] = x.l;
         __syncthreads();
         if (tid < items) {
-            const int used = (int)((last - first) / step) + 1 < lots ? (int)((last - first) / step) + 1 : lots;
-            for (int k = 1; k < used; ++k) x.add(sm[tid + k * items], sl[tid + k * items], sv[2 * (tid + k * items)], sv[2 * (tid + k * items) + 1]);
+            x.clear();
+            x.add<kLots>((1u << lots) - 1, [&](int k, float &m, float &l, F4 &lo, F4 &hi) {
+                const int at = k < lots ? tid + k * items : tid;
+                m = sm[at]; l = sl[at]; lo = sv[2 * at]; hi = sv[2 * at + 1];
+            });
         }
     }
     __syncthreads();                             // all parts are read, and LDS is free again
@@ -436,37 +511,33 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     const uint32_t hc = (uint32_t)(a.kv_heads * a.chunks);
     const int rows = a.group < kQueries ? a.group : kQueries;            // of a slot in LDS
 
-    // the units of all sequences, 64 sequences at a time
+    // the units of all sequences, 64 sequences at a time; the first 64 stay
+    Place pl;
+    const auto units_upto = [&](int c) {
+        pl.lanes(a, c, lane);
+        return sums_upto(64 * c + lane < a.batch ? (uint32_t)span_of(a, pl.length).units : 0u);
+    };
     uint32_t total = 0;
-#pragma unroll 4
-    for (int c = 0; c < (a.batch + 63) / 64; ++c) {
-        const int i = c * 64 + lane;
-        const int n = a.lengths[i < a.batch ? i : a.batch - 1];
-        total += i < a.batch ? (uint32_t)span_of(a, n).units : 0u;
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-    total = (uint32_t)__builtin_amdgcn_readfirstlane((int)total) * hc;
-    const uint32_t mine = (total + gridDim.x * WAVES - 1) / (gridDim.x * WAVES), share = mine * WAVES;
+    for (int c = (a.batch - 1) >> 6; c > 0; --c) total += (uint32_t)__builtin_amdgcn_readlane((int)units_upto(c), 63);
+    uint32_t upto = units_upto(0);
+    total = (total + (uint32_t)__builtin_amdgcn_readlane((int)upto, 63)) * hc;
+    // Units of a block and of a wave: all waves of the grid alike; where that would leave a block fewer than kLeastUnits, fewer blocks.
+    uint32_t share = quotient(total + gridDim.x - 1, gridDim.x, a.per_block), mine = 1;
+    if (share < kLeastUnits) share = kLeastUnits;
+    if (share >= WAVES) { mine = (share + WAVES - 1) / WAVES; share = mine * WAVES; }
     const uint32_t begin = blockIdx.x * share;
     if (begin >= total) return;
     const uint32_t end = begin + share < total ? begin + share : total;
     const uint32_t wbegin = begin + wave * mine, wend = wbegin + mine < end ? wbegin + mine : end;
+    const float per_share = 1.0f / (float)share;
 
     const int n = lane & 15, quarter = lane >> 4;
-    if (lane < 2) s_seg[wave][lane].on = 0;
-    if (tid < 2) { s_last[tid] = 0; s_out[tid].on = 0; }
-    if (wbegin < wend) {
-        Place pl;
+    if (lane < 2) s_seg[wave][lane].seg1 = 0;
+    if (tid < 2) s_last[tid] = 0;
+    const bool busy = wbegin < wend;
+    if (busy) {
         pl.base = 0;
-        for (int c = 0;; ++c) {                  // the sequence that holds unit wbegin
-            pl.lanes(a, c, lane);
-            uint32_t upto = 64 * c + lane < a.batch ? (uint32_t)span_of(a, pl.length).units : 0u;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t x = __shfl_up(upto, d);
-                if (lane >= d) upto += x;
-            }
+        for (int c = 0;;) {                      // the sequence that holds unit wbegin
             const int before = __popcll(__ballot(pl.base + upto * hc <= wbegin));
             if (before < 64) {
                 if (before) pl.base += (uint32_t)__builtin_amdgcn_readlane((int)upto, before - 1) * hc;
@@ -474,46 +545,58 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                 break;
             }
             pl.base += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
+            upto = units_upto(++c);
         }
-        Head h;
-        h.page_log = a.page_log;
-        h.kv_heads = a.kv_heads;
-        h.bytes = (uint32_t)(D * EB) << a.page_log;
-        h.page_bytes = (int64_t)h.bytes * a.kv_heads;
-
-        uint32_t at = wbegin;
-        while (at < wend) {
-            while (pl.base + (uint32_t)pl.sp.units * hc <= at) pl.next(a, lane, hc);
-            const int seg = (int)((at - pl.base) / (uint32_t)pl.sp.units);
-            const uint32_t seg0 = pl.base + (uint32_t)seg * pl.sp.units, seg1 = seg0 + pl.sp.units;
-            const uint32_t stop = seg1 < wend ? seg1 : wend;
-            const int u0 = pl.sp.unit0 + (int)(at - seg0), u1 = pl.sp.unit0 + (int)(stop - seg0), lo = pl.sp.lo, hi = pl.sp.hi;
-            const Target to(a, pl.b, seg, D);
-            h.head = seg / a.chunks;
-            h.at = (int64_t)h.bytes * h.head;
-
+    }
+    Head h;
+    h.page_log = a.page_log;
+    h.kv_heads = a.kv_heads;
+    h.bytes = (uint32_t)(D * EB) << a.page_log;
+    h.page_bytes = (int64_t)h.bytes * a.kv_heads;
+    Segment g;                                   // the segment at hand: units u0..u1 of it, tokens lo..hi of its sequence
+    int u0, u1, lo, hi, pages = 0;
+    const int32_t *row;
+    Target to;
+    half8v q[D / 32];
+    // the pages of the next 32 units, two halves to a unit
+    const auto turn = [&](int u) {
+        int t = (u + (lane >> 1)) * kUnit + (lane & 1) * 16;
+        t = t < hi ? t : hi - 1;
+        pages = hi > 0 ? row[t >> a.page_log] : 0;
+        if ((uint32_t)pages >= (uint32_t)a.n_pages) pages = -1;
+    };
+    const auto locate = [&](uint32_t at) {
+        while (pl.base + (uint32_t)pl.sp.units * hc <= at) pl.next(a, lane, hc);
+        lo = pl.sp.lo; hi = pl.sp.hi;
+        row = a.table + (int64_t)pl.b * a.ld_table;
+        const uint32_t units = (uint32_t)pl.sp.units;
+        g.b = pl.b;
+        g.seg = (int)quotient(at - pl.base, units, 1.0f / (float)units);
+        g.seg0 = pl.base + (uint32_t)g.seg * units;
+        g.seg1 = g.seg0 + units;
+        u0 = pl.sp.unit0 + (int)(at - g.seg0);
+        u1 = pl.sp.unit0 + (int)((g.seg1 < wend ? g.seg1 : wend) - g.seg0);
+        turn(u0);
+        to = Target(a, g.b, g.seg, D);
+        h.head = to.head;
+        h.at = (int64_t)h.bytes * h.head;
+        const _Float16 *qp = a.q + (int64_t)g.b * a.ldq + (int64_t)(to.first + (n < to.queries ? n : 0)) * D;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s)
+            q[s] = *(const half8v *)(qp + (FMT == 0 ? s * 32 + quarter * 8 : ((s >> 1) * 4 + quarter) * 16 + (s & 1) * 8));
+    };
+    if (busy) locate(wbegin);
+    __syncthreads();                             // every wave has asked for its pages before the first keys fill the way to memory
+    if (busy) {
+        for (uint32_t at = wbegin;;) {
+            const uint32_t stop = g.seg1 < wend ? g.seg1 : wend;
             Running<D> st;
             st.clear();
             if (hi > 0) {
-                const int32_t *row = a.table + (int64_t)pl.b * a.ld_table;
-                int pages = 0;
-                // the pages of the next 32 units, two halves to a unit
-                const auto turn = [&](int u) {
-                    int t = (u + (lane >> 1)) * kUnit + (lane & 1) * 16;
-                    t = t < hi ? t : hi - 1;
-                    pages = row[t >> a.page_log];
-                    if ((uint32_t)pages >= (uint32_t)a.n_pages) pages = -1;
-                };
                 const auto page_of = [&](int (&pg)[2], int i) {
 #pragma unroll
                     for (int z = 0; z < 2; ++z) pg[z] = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + z);
                 };
-                half8v q[D / 32];
-                const _Float16 *qp = a.q + (int64_t)pl.b * a.ldq + (to.o - (int64_t)pl.b * a.ldo) + (int64_t)(n < to.queries ? n : 0) * D;
-#pragma unroll
-                for (int s = 0; s < D / 32; ++s)
-                    q[s] = *(const half8v *)(qp + (FMT == 0 ? s * 32 + quarter * 8 : ((s >> 1) * 4 + quarter) * 16 + (s & 1) * 8));
-                turn(u0);
                 int pg[2];
                 page_of(pg, 0);
                 Keys<D, FMT> k;
@@ -533,7 +616,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                 }
             }
             const float l = sum4(st.l);
-            if (at == seg0 && stop == seg1) {    // all of the segment is here
+            if (at == g.seg0 && stop == g.seg1) {        // all of the segment is here
                 if (n < to.queries) {
                     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                     _Float16 *o = a.o + to.o + (int64_t)n * D + quarter * 4 * R;
@@ -555,8 +638,8 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                     if (a.lse && quarter == 0) a.lse[to.lse + n] = lse_of(st.m, l);
                 }
             } else {
-                const int slot = 2 * wave + (seg0 >= wbegin);            // the segment that goes on from before, or the one that goes on after
-                if (lane == 0) s_seg[wave][seg0 >= wbegin] = {1, pl.b, seg, seg0, seg1};
+                const int slot = 2 * wave + (g.seg0 >= wbegin);          // the segment that goes on from before, or the one that goes on after
+                if (lane == 0) s_seg[wave][g.seg0 >= wbegin] = g;
                 if (quarter == 0) { s_m[slot * kQueries + n] = st.m; s_l[slot * kQueries + n] = l; }
                 if (n < to.queries) {
                     float *o = s_o + (slot * rows + n) * kRow + quarter * 4 * R;
@@ -567,6 +650,8 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                 }
             }
             at = stop;
+            if (at >= wend) break;
+            locate(at);
         }
     }
     __syncthreads();
@@ -574,33 +659,32 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     // segments that began with a wave's last units (or before the block) and go on: joined by that wave over the waves behind
     const __amdgpu_buffer_rsrc_t parts = attn_rsrc(a.partial, 2 * kAttnBlocks * part_floats<D>() * 4);
     for (int z = wave == 0 ? 0 : 1; z < 2; ++z) {
-        const Segment g = s_seg[wave][z];
-        if (!g.on) continue;
-        int wl = wave;
-        while (wl + 1 < WAVES && s_seg[wl + 1][0].on && s_seg[wl + 1][0].seg0 == g.seg0) ++wl;
+        const Segment g = s_seg[wave][z].uniform();
+        if (!g.seg1) continue;
+        // the waves behind whose first units go on with it: a run of lanes, lane w for wave w
+        const Segment other = s_seg[lane % WAVES][0];
+        const uint32_t behind = (uint32_t)__ballot(lane > wave && lane < WAVES && other.seg1 && other.seg0 == g.seg0);
+        const uint32_t which = behind | 1u << wave;
         const Target to(a, g.b, g.seg, D);
         const bool whole = g.seg0 >= begin && g.seg1 <= end;
         for (int i = lane; i < to.queries * (D / 8); i += 64) {
             const int query = i / (D / 8), channel = (i % (D / 8)) * 8;
             Eight x;
             x.clear();
-            for (int w = wave; w <= wl; ++w) {
+            x.add<WAVES>(which, [&](int w, float &m, float &l, F4 &lo, F4 &hi) {
                 const int slot = 2 * w + (w == wave ? z : 0);
                 const float *o = s_o + (slot * rows + query) * kRow + channel;
-                x.add(s_m[slot * kQueries + query], s_l[slot * kQueries + query], *(const F4 *)o, *(const F4 *)(o + 4));
-            }
+                m = s_m[slot * kQueries + query]; l = s_l[slot * kQueries + query]; lo = *(const F4 *)o; hi = *(const F4 *)(o + 4);
+            });
             if (whole) x.result(a, to, D, query, channel);
             else store_part<D>(parts, 2 * blockIdx.x + (g.seg0 >= begin), query, channel, x);
         }
         if (!whole) {
+            const Sharers by(g, share, per_share, blockIdx.x);
+            uint32_t *counter = by.in_groups ? a.arrived + 2 * by.group + (g.seg0 >= by.group * share) : a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg;
             stores_done();
             if (lane == 0) {
-                const uint32_t first = g.seg0 / share, last = (g.seg1 - 1) / share, all = last - first + 1;
-                const uint32_t group = (blockIdx.x - first) / kGroupParts * kGroupParts + first;
-                const bool in_groups = all > kGroupParts;
-                uint32_t *counter = in_groups ? a.arrived + 2 * group + (g.seg0 >= group * share) : a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg;
-                const uint32_t of = in_groups ? (last - group + 1 < kGroupParts ? last - group + 1 : kGroupParts) : all;
-                s_last[g.seg0 >= begin] = arrives_last(counter, of);
+                s_last[g.seg0 >= begin] = arrives_last(counter, by.in_groups ? by.group_last - by.group + 1 : by.last - by.first + 1);
                 s_out[g.seg0 >= begin] = g;
             }
         }
@@ -609,31 +693,28 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
 
     // the segments shared with other blocks whose last share has now arrived
     for (int z = 0; z < 2; ++z) {
-        if (!s_last[z]) continue;
-        const Segment g = s_out[z];
+        if (!__builtin_amdgcn_readfirstlane(s_last[z])) continue;
+        const Segment g = s_out[z].uniform();
         const Target to(a, g.b, g.seg, D);
-        const uint32_t first = g.seg0 / share, last = (g.seg1 - 1) / share;
+        const Sharers by(g, share, per_share, blockIdx.x);
         const int items = to.queries * (D / 8);
-        const bool in_groups = last - first + 1 > kGroupParts;
-        bool final = !in_groups;
-        if (in_groups) {                         // the group's result takes the place of its first part
-            const uint32_t group = (blockIdx.x - first) / kGroupParts * kGroupParts + first;
-            const uint32_t of = group + kGroupParts - 1 < last ? group + kGroupParts - 1 : last;
+        bool final = !by.in_groups;
+        if (by.in_groups) {                      // the group's result takes the place of its first part
             for (int i0 = 0; i0 < items; i0 += THREADS) {
                 const int some = items - i0 < THREADS ? items - i0 : THREADS;
-                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, group, 1, of, i0, some, tid);
-                if (tid < some) store_part<D>(parts, 2 * group + (g.seg0 >= group * share), (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8, x);
+                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, by.group, 1, by.group_last, i0, some, tid);
+                if (tid < some) store_part<D>(parts, 2 * by.group + (g.seg0 >= by.group * share), (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8, x);
             }
             stores_done();
             __syncthreads();
-            if (tid == 0) s_last[z] = arrives_last(a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg, (last - first) / kGroupParts + 1);
+            if (tid == 0) s_last[z] = arrives_last(a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg, (by.last - by.first) / kGroupParts + 1);
             __syncthreads();
-            final = s_last[z];
+            final = __builtin_amdgcn_readfirstlane(s_last[z]);
         }
         if (final)
             for (int i0 = 0; i0 < items; i0 += THREADS) {
                 const int some = items - i0 < THREADS ? items - i0 : THREADS;
-                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, first, in_groups ? kGroupParts : 1, last, i0, some, tid);
+                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, by.first, by.in_groups ? kGroupParts : 1, by.last, i0, some, tid);
                 if (tid < some) x.result(a, to, D, (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8);
             }
     }
@@ -644,11 +725,13 @@ static size_t attn_part_bytes(const paro_kv_cache &c) { return sizeof(float) * k
 static size_t attn_scratch_bytes(const paro_kv_cache &c) { return ((size_t)2 * kAttnBlocks * attn_part_bytes(c) + 255) / 256 * 256; }
 
 template <int D, int FMT>
-static hipError_t launch_attention(const AttnArgs &a, int64_t units, hipStream_t s)
+static hipError_t launch_attention(AttnArgs &a, int64_t units, hipStream_t s)
 {
     constexpr int WAVES = attn_waves<D>();
-    // no more waves than the longest sequences could have units
-    const int64_t blocks = (units + WAVES - 1) / WAVES;
+    // no more blocks than the longest sequences could have units for
+    const int64_t most = (units + kLeastUnits - 1) / kLeastUnits;
+    const unsigned blocks = (unsigned)(most < kAttnBlocks ? most : kAttnBlocks);
+    a.per_block = 1.0f / (float)blocks;
     const int rows = a.group < kQueries ? a.group : kQueries;
     const size_t shares = sizeof(float) * WAVES * 2 * rows * (D + 4), joins = sizeof(float) * 10 * 64 * WAVES;
     static std::atomic<uint64_t> attr_done{0};
@@ -658,7 +741,7 @@ static hipError_t launch_attention(const AttnArgs &a, int64_t units, hipStream_t
         if (e != hipSuccess) return e;
         once_done(attr_done, dev);
     }
-    hipLaunchKernelGGL((paged_attention_kernel<D, FMT>), dim3((unsigned)(blocks < kAttnBlocks ? blocks : kAttnBlocks)), dim3(64 * WAVES),
+    hipLaunchKernelGGL((paged_attention_kernel<D, FMT>), dim3(blocks), dim3(64 * WAVES),
                        shares > joins ? shares : joins, s, a);
     return hipGetLastError();
 }
@@ -696,6 +779,7 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     if (!aligned(block_table, 4) || !aligned(lengths, 4) || (lse && !aligned(lse, 4))) return PARO_ERR_ALIGN;
     // units are numbered with 32 bits, and so are a sequence's tokens
     const int64_t tokens = (int64_t)table_width * c.page;
+    if (q_heads > 65535) return PARO_ERR_UNSUPPORTED;
     const int64_t units = (int64_t)batch * c.kv_heads * attn_chunks(c, q_heads);
     if (tokens > (int64_t)1 << 30 || units > (int64_t)1 << 30 || units * ((tokens + kUnit - 1) / kUnit) > (int64_t)1 << 30) return PARO_ERR_UNSUPPORTED;
     const size_t scratch = attn_scratch_bytes(c);
