@@ -383,103 +383,91 @@ struct Sharers {
     }
 };
 
-// 8 channels of one query, with the maximum and sum that belong to them
-struct Eight {
-    float m, l, v[8];
-    __device__ void clear()
-    {
-        m = -INFINITY; l = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0;
-    }
-    // Takes in those of N results that `which` has a bit for; all are read first.
+// 4 channels of one query, with the maximum and sum that belong to them
+struct Four {
+    float m, l;
+    F4 v;
+    __device__ void clear() { m = -INFINITY; l = 0; v = F4{0, 0, 0, 0}; }
+    // Takes in N results; read(k) gives -inf, 0 and anything finite for one that is not there, all before any is used.
     template <int N, class Read>
-    __device__ void add(uint32_t which, Read read)
+    __device__ void add(Read read)
     {
         float pm[N], pl[N], top = m;
-        F4 lo[N], hi[N];
+        F4 pv[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) read(k, pm[k], pl[k], lo[k], hi[k]);
+        for (int k = 0; k < N; ++k) read(k, pm[k], pl[k], pv[k]);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (which >> k & 1) top = fmaxf(top, pm[k]);
+        for (int k = 0; k < N; ++k) top = fmaxf(top, pm[k]);
         const float ref = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - ref);
         l *= f;
+        v *= f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= f;
+        for (int k = 0; k < N; ++k) {
+            const float g = __builtin_amdgcn_exp2f(pm[k] - ref);
+            l = fmaf(pl[k], g, l);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (which >> k & 1) {
-                const float g = __builtin_amdgcn_exp2f(pm[k] - ref);
-                l = fmaf(pl[k], g, l);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = fmaf(e < 4 ? lo[k][e & 3] : hi[k][e & 3], g, v[e]);
-            }
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(pv[k][e], g, v[e]);
+        }
         m = top;
     }
     __device__ void result(const AttnArgs &a, const Target &to, int D, int query, int channel) const
     {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        half8v h;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = (_Float16)(v[e] * inv);
-        *(half8v *)(a.o + to.o + (int64_t)query * D + channel) = h;
+        const float inv = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
+        *(half4v *)(a.o + to.o + query * D + channel) = half4v{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
         if (a.lse && channel == 0) a.lse[to.lse + query] = lse_of(m, l);
     }
 };
 
 template <int D> constexpr int part_floats() { return kQueries * (D + 4); }
-// Eight of the partial result in slot `slot`, through memory that all XCDs see
+// Four of the partial result in slot `slot`, through memory that all XCDs see
 template <int D>
-__device__ inline void store_part(__amdgpu_buffer_rsrc_t r, uint32_t slot, int query, int channel, const Eight &x)
+__device__ inline void store_part(__amdgpu_buffer_rsrc_t r, uint32_t slot, int query, int channel, const Four &x)
 {
     const uint32_t row = (slot * part_floats<D>() + query * (D + 4)) * 4u;
     typedef decltype(__builtin_amdgcn_raw_buffer_load_b128(r, 0, 0, 0)) B4;
     typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(r, 0, 0, 0)) B2;
     if (channel == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B2, U2{__float_as_uint(x.m), __float_as_uint(x.l)}), r, row, 0, kAgent);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{x.v[0], x.v[1], x.v[2], x.v[3]}), r, row + (4 + channel) * 4u, 0, kAgent);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{x.v[4], x.v[5], x.v[6], x.v[7]}), r, row + (8 + channel) * 4u, 0, kAgent);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, x.v), r, row + (4 + channel) * 4u, 0, kAgent);
 }
 
 // Joins the partial results of blocks first, first + step, ... last of a segment, by the whole block: thread tid < items gets
-// the Eight of item0 + tid.  s: LDS of 10 floats per thread.
+// the Four of item0 + tid.  s: LDS of 6 floats per thread.
 template <int D, int THREADS>
-__device__ inline Eight join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Segment &g, uint32_t share, uint32_t first, uint32_t step, uint32_t last,
-                                   int item0, int items, int tid)
+__device__ inline Four join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Segment &g, uint32_t share, uint32_t first, uint32_t step, uint32_t last,
+                                  int item0, int items, int tid)
 {
     // `lots` groups of threads take every lots-th part
-    constexpr int kLots = 8, kBatch = 4;
-    const int lots = THREADS / items < kLots ? THREADS / items : kLots;
-    const int lot = tid / items, i = item0 + tid - lot * items, query = i / (D / 8), channel = (i % (D / 8)) * 8;
-    Eight x;
+    constexpr int kLots = 4, kBatch = 4;
+    int lots = THREADS / items;
+    lots = lots < kLots ? lots : kLots;
+    const int lot = tid / items, i = item0 + tid - lot * items, query = i / (D / 4), channel = (i % (D / 4)) * 4;
+    Four x;
     x.clear();
     if (lot < lots)
-        for (uint32_t j = first + lot * step; j <= last; j += kBatch * lots * step) {
-            const uint32_t left = (last - j) / (lots * step) + 1;
-            x.add<kBatch>((1u << (left < kBatch ? left : kBatch)) - 1, [&](int z, float &m, float &l, F4 &lo, F4 &hi) {
+        for (uint32_t j = first + lot * step; j <= last; j += kBatch * lots * step)
+            x.add<kBatch>([&](int z, float &m, float &l, F4 &v) {
                 const uint32_t k = j + z * lots * step;
-                // past the last one: a request beyond the buffer
+                // past the last one: a request beyond the buffer, which gives zeros
                 const uint32_t row = k <= last ? ((2 * k + (g.seg0 >= k * share)) * part_floats<D>() + query * (D + 4)) * 4u : 0x80000000u;
                 const U2 ml = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, row, 0, kAgent));
-                m = __uint_as_float(ml[0]);
+                v = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
+                m = k <= last ? __uint_as_float(ml[0]) : -INFINITY;
                 l = __uint_as_float(ml[1]);
-                lo = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
-                hi = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (8 + channel) * 4u, 0, kAgent));
             });
-        }
     if (lots > 1) {
         F4 *sv = (F4 *)s;
-        float *sm = s + 8 * THREADS, *sl = sm + THREADS;
-        sv[2 * tid] = F4{x.v[0], x.v[1], x.v[2], x.v[3]};
-        sv[2 * tid + 1] = F4{x.v[4], x.v[5], x.v[6], x.v[7]};
-        sm[tid] = x.m;
-        sl[tid] = x.l;
+        U2 *sm = (U2 *)(s + 4 * THREADS);
+        sv[tid] = x.v;
+        sm[tid] = U2{__float_as_uint(x.m), __float_as_uint(x.l)};
         __syncthreads();
         if (tid < items) {
             x.clear();
-            x.add<kLots>((1u << lots) - 1, [&](int k, float &m, float &l, F4 &lo, F4 &hi) {
+            x.add<kLots>([&](int k, float &m, float &l, F4 &v) {
                 const int at = k < lots ? tid + k * items : tid;
-                m = sm[at]; l = sl[at]; lo = sv[2 * at]; hi = sv[2 * at + 1];
+                const U2 ml = sm[at];
+                v = sv[at];
+                m = k < lots ? __uint_as_float(ml[0]) : -INFINITY;
+                l = __uint_as_float(ml[1]);
             });
         }
     }
@@ -563,7 +551,6 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         int t = (u + (lane >> 1)) * kUnit + (lane & 1) * 16;
         t = t < hi ? t : hi - 1;
         pages = hi > 0 ? row[t >> a.page_log] : 0;
-        if ((uint32_t)pages >= (uint32_t)a.n_pages) pages = -1;
     };
     const auto locate = [&](uint32_t at) {
         while (pl.base + (uint32_t)pl.sp.units * hc <= at) pl.next(a, lane, hc);
@@ -595,7 +582,10 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
             if (hi > 0) {
                 const auto page_of = [&](int (&pg)[2], int i) {
 #pragma unroll
-                    for (int z = 0; z < 2; ++z) pg[z] = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + z);
+                    for (int z = 0; z < 2; ++z) {
+                        const int p = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + z);
+                        pg[z] = (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
+                    }
                 };
                 int pg[2];
                 page_of(pg, 0);
@@ -618,7 +608,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
             const float l = sum4(st.l);
             if (at == g.seg0 && stop == g.seg1) {        // all of the segment is here
                 if (n < to.queries) {
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                    const float inv = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
                     _Float16 *o = a.o + to.o + (int64_t)n * D + quarter * 4 * R;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -667,14 +657,18 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         const uint32_t which = behind | 1u << wave;
         const Target to(a, g.b, g.seg, D);
         const bool whole = g.seg0 >= begin && g.seg1 <= end;
-        for (int i = lane; i < to.queries * (D / 8); i += 64) {
-            const int query = i / (D / 8), channel = (i % (D / 8)) * 8;
-            Eight x;
+        for (int i = lane; i < to.queries * (D / 4); i += 64) {
+            const int query = i / (D / 4), channel = (i % (D / 4)) * 4;
+            Four x;
             x.clear();
-            x.add<WAVES>(which, [&](int w, float &m, float &l, F4 &lo, F4 &hi) {
-                const int slot = 2 * w + (w == wave ? z : 0);
-                const float *o = s_o + (slot * rows + query) * kRow + channel;
-                m = s_m[slot * kQueries + query]; l = s_l[slot * kQueries + query]; lo = *(const F4 *)o; hi = *(const F4 *)(o + 4);
+            x.add<WAVES>([&](int w, float &m, float &l, F4 &v) {
+                // a wave that has no share: this one's values, with no weight
+                const bool on = which >> w & 1;
+                const int slot = 2 * (on ? w : wave) + (on && w != wave ? 0 : z);
+                m = s_m[slot * kQueries + query];
+                m = on ? m : -INFINITY;
+                l = s_l[slot * kQueries + query];
+                v = *(const F4 *)(s_o + (slot * rows + query) * kRow + channel);
             });
             if (whole) x.result(a, to, D, query, channel);
             else store_part<D>(parts, 2 * blockIdx.x + (g.seg0 >= begin), query, channel, x);
@@ -697,13 +691,13 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         const Segment g = s_out[z].uniform();
         const Target to(a, g.b, g.seg, D);
         const Sharers by(g, share, per_share, blockIdx.x);
-        const int items = to.queries * (D / 8);
+        const int items = to.queries * (D / 4);
         bool final = !by.in_groups;
         if (by.in_groups) {                      // the group's result takes the place of its first part
             for (int i0 = 0; i0 < items; i0 += THREADS) {
                 const int some = items - i0 < THREADS ? items - i0 : THREADS;
-                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, by.group, 1, by.group_last, i0, some, tid);
-                if (tid < some) store_part<D>(parts, 2 * by.group + (g.seg0 >= by.group * share), (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8, x);
+                const Four x = join_parts<D, THREADS>(parts, s_o, g, share, by.group, 1, by.group_last, i0, some, tid);
+                if (tid < some) store_part<D>(parts, 2 * by.group + (g.seg0 >= by.group * share), (i0 + tid) / (D / 4), ((i0 + tid) % (D / 4)) * 4, x);
             }
             stores_done();
             __syncthreads();
@@ -714,8 +708,8 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         if (final)
             for (int i0 = 0; i0 < items; i0 += THREADS) {
                 const int some = items - i0 < THREADS ? items - i0 : THREADS;
-                const Eight x = join_parts<D, THREADS>(parts, s_o, g, share, by.first, by.in_groups ? kGroupParts : 1, by.last, i0, some, tid);
-                if (tid < some) x.result(a, to, D, (i0 + tid) / (D / 8), ((i0 + tid) % (D / 8)) * 8);
+                const Four x = join_parts<D, THREADS>(parts, s_o, g, share, by.first, by.in_groups ? kGroupParts : 1, by.last, i0, some, tid);
+                if (tid < some) x.result(a, to, D, (i0 + tid) / (D / 4), ((i0 + tid) % (D / 4)) * 4);
             }
     }
 }
@@ -733,7 +727,7 @@ static hipError_t launch_attention(AttnArgs &a, int64_t units, hipStream_t s)
     const unsigned blocks = (unsigned)(most < kAttnBlocks ? most : kAttnBlocks);
     a.per_block = 1.0f / (float)blocks;
     const int rows = a.group < kQueries ? a.group : kQueries;
-    const size_t shares = sizeof(float) * WAVES * 2 * rows * (D + 4), joins = sizeof(float) * 10 * 64 * WAVES;
+    const size_t shares = sizeof(float) * WAVES * 2 * rows * (D + 4), joins = sizeof(float) * 6 * 64 * WAVES;
     static std::atomic<uint64_t> attr_done{0};
     if (const int dev = once_pending(attr_done); dev >= 0) {
         const hipError_t e = hipFuncSetAttribute((const void *)paged_attention_kernel<D, FMT>, hipFuncAttributeMaxDynamicSharedMemorySize,
