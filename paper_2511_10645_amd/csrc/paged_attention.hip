@@ -347,10 +347,10 @@ __device__ inline uint32_t quotient(uint32_t x, uint32_t d, float inv)
 struct Segment {
     int b, seg;
     uint32_t seg0, seg1;                         // seg1 0: none
-    __device__ Segment uniform() const           // as read from LDS, in scalar registers
+    __device__ Segment of_lane(int i) const
     {
-        return {__builtin_amdgcn_readfirstlane(b), __builtin_amdgcn_readfirstlane(seg), (uint32_t)__builtin_amdgcn_readfirstlane((int)seg0),
-                (uint32_t)__builtin_amdgcn_readfirstlane((int)seg1)};
+        return {__builtin_amdgcn_readlane(b, i), __builtin_amdgcn_readlane(seg, i), (uint32_t)__builtin_amdgcn_readlane((int)seg0, i),
+                (uint32_t)__builtin_amdgcn_readlane((int)seg1, i)};
     }
 };
 struct Target {
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     constexpr int kRow = D + 4;                  // floats of a row in LDS: rows of 16 queries fall on distinct banks
     extern __shared__ __attribute__((aligned(16))) float s_o[];          // [wave][2][rows][kRow], later the joins'
     __shared__ float s_m[WAVES * 2 * kQueries], s_l[WAVES * 2 * kQueries];
-    __shared__ Segment s_seg[WAVES][2], s_out[2];
+    __shared__ Segment s_seg[WAVES][2];
     __shared__ int s_last[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t hc = (uint32_t)(a.kv_heads * a.chunks);
@@ -646,49 +646,62 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     }
     __syncthreads();
 
-    // segments that began with a wave's last units (or before the block) and go on: joined by that wave over the waves behind
+    // Lane 2 w + z has what slot z of wave w holds.  A chain is a segment's slots in this block: one that goes on after its wave
+    // began it, or wave 0's from before, and the first slots of the waves behind.  The chains are dealt to teams of waves, a
+    // thread for every item of a chain.
     const __amdgpu_buffer_rsrc_t parts = attn_rsrc(a.partial, 2 * kAttnBlocks * part_floats<D>() * 4);
-    for (int z = wave == 0 ? 0 : 1; z < 2; ++z) {
-        const Segment g = s_seg[wave][z].uniform();
-        if (!g.seg1) continue;
-        // the waves behind whose first units go on with it: a run of lanes, lane w for wave w
-        const Segment other = s_seg[lane % WAVES][0];
-        const uint32_t behind = (uint32_t)__ballot(lane > wave && lane < WAVES && other.seg1 && other.seg0 == g.seg0);
-        const uint32_t which = behind | 1u << wave;
+    const Segment held = s_seg[lane / 2 % WAVES][lane & 1];
+    const bool there = lane < 2 * WAVES && held.seg1 != 0;
+    const uint32_t starts = (uint32_t)__ballot(there && (lane & 1 || lane == 0));
+    const int team_waves = rows * (D / 4) <= 64 ? 1 : rows * (D / 4) <= 128 ? 2 : rows * (D / 4) <= 256 ? 4 : 8;
+    const int teams = WAVES >= team_waves ? WAVES / team_waves : 1, team = wave / team_waves;
+    int turn_of = 0;
+    for (uint32_t left = starts; left; left &= left - 1) {
+        if (turn_of++ % teams != team) continue;
+        const int slot0 = __builtin_ctz(left);
+        const Segment g = held.of_lane(slot0);
+        const uint32_t behind = (uint32_t)__ballot(there && !(lane & 1) && lane > slot0 && held.seg0 == g.seg0);
+        const int links = 1 + __builtin_popcount(behind);
         const Target to(a, g.b, g.seg, D);
         const bool whole = g.seg0 >= begin && g.seg1 <= end;
-        for (int i = lane; i < to.queries * (D / 4); i += 64) {
+        for (int i = tid - team * team_waves * 64; i < to.queries * (D / 4); i += team_waves * 64 < THREADS ? team_waves * 64 : THREADS) {
             const int query = i / (D / 4), channel = (i % (D / 4)) * 4;
             Four x;
             x.clear();
-            x.add<WAVES>([&](int w, float &m, float &l, F4 &v) {
-                // a wave that has no share: this one's values, with no weight
-                const bool on = which >> w & 1;
-                const int slot = 2 * (on ? w : wave) + (on && w != wave ? 0 : z);
-                m = s_m[slot * kQueries + query];
-                m = on ? m : -INFINITY;
-                l = s_l[slot * kQueries + query];
-                v = *(const F4 *)(s_o + (slot * rows + query) * kRow + channel);
-            });
+            for (int k0 = 0; k0 < links; k0 += 4)
+                x.add<4>([&](int k, float &m, float &l, F4 &v) {
+                    // past the last link: the first one again, with no weight
+                    const bool on = k0 + k < links;
+                    const int slot = on && k0 + k ? (slot0 & ~1) + 2 * (k0 + k) : slot0;
+                    m = s_m[slot * kQueries + query];
+                    m = on ? m : -INFINITY;
+                    l = s_l[slot * kQueries + query];
+                    v = *(const F4 *)(s_o + (slot * rows + query) * kRow + channel);
+                });
             if (whole) x.result(a, to, D, query, channel);
             else store_part<D>(parts, 2 * blockIdx.x + (g.seg0 >= begin), query, channel, x);
         }
-        if (!whole) {
-            const Sharers by(g, share, per_share, blockIdx.x);
-            uint32_t *counter = by.in_groups ? a.arrived + 2 * by.group + (g.seg0 >= by.group * share) : a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg;
-            stores_done();
-            if (lane == 0) {
-                s_last[g.seg0 >= begin] = arrives_last(counter, by.in_groups ? by.group_last - by.group + 1 : by.last - by.first + 1);
-                s_out[g.seg0 >= begin] = g;
-            }
-        }
+    }
+    if (!starts) return;
+
+    // Segments shared with other blocks: the one from before this block and the one that goes on after it.
+    const Segment from = held.of_lane(__builtin_ctz(starts)), on = held.of_lane(31 - __builtin_clz(starts));
+    const bool from_before = from.seg0 < begin, goes_on = on.seg0 >= begin && on.seg1 > end;
+    if (!from_before && !goes_on) return;
+    stores_done();
+    __syncthreads();
+    if (tid == 0 ? from_before : tid == 64 && goes_on) {
+        const Segment g = wave == 0 ? from : on;
+        const Sharers by(g, share, per_share, blockIdx.x);
+        uint32_t *counter = by.in_groups ? a.arrived + 2 * by.group + (g.seg0 >= by.group * share) : a.arrived + 2 * kAttnBlocks + (size_t)g.b * hc + g.seg;
+        s_last[wave] = arrives_last(counter, by.in_groups ? by.group_last - by.group + 1 : by.last - by.first + 1);
     }
     __syncthreads();
 
-    // the segments shared with other blocks whose last share has now arrived
+    // those whose last share has now arrived
     for (int z = 0; z < 2; ++z) {
         if (!__builtin_amdgcn_readfirstlane(s_last[z])) continue;
-        const Segment g = s_out[z].uniform();
+        const Segment g = z == 0 ? from : on;
         const Target to(a, g.b, g.seg, D);
         const Sharers by(g, share, per_share, blockIdx.x);
         const int items = to.queries * (D / 4);
