@@ -3,6 +3,8 @@
 // the 3.3 of the call itself (the output alone 1.7, the checks of rows and strides 0.5, the stream's handle 0.4).
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -154,10 +156,17 @@ bool maybe(PyObject *o, const at::Tensor *&t)
     t = nullptr;
     return o == Py_None || (t = tensor(o));
 }
+// A new dense tensor where `like` is, from the allocator that `like` came from: 0.3 us of host time, 0.85 by way of the dispatcher.
+at::Tensor fresh(const at::Tensor &like, at::IntArrayRef sizes, at::ScalarType type)
+{
+    c10::Allocator *allocator = like.storage().allocator();
+    if (!allocator || like.device().index() != c10::hip::current_device()) return at::empty(sizes, like.options().dtype(type).requires_grad(false));
+    return at::Tensor(at::detail::empty_generic(sizes, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));
+}
 // `o` if given, else new rows; undefined with an exception set on failure
 at::Tensor rows_or_new(PyObject *o, int64_t t, int64_t width, const at::Tensor &like)
 {
-    if (o == Py_None) return at::empty({t, width}, like.options().requires_grad(false));
+    if (o == Py_None) return fresh(like, {t, width}, at::kHalf);
     const at::Tensor *x = tensor(o);
     return x && gpu_rows(*x, t, width) ? *x : at::Tensor();
 }
@@ -216,8 +225,8 @@ PyObject *rms_norm_quantize_e4m3(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (PyErr_Occurred() || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
     at::Tensor h;
     if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
-    at::Tensor codes = at::empty({T, C}, x->options().dtype(at::kByte).requires_grad(false));
-    at::Tensor scales = at::empty({T, group > 0 ? C / group : 1}, x->options().dtype(at::kFloat).requires_grad(false));
+    at::Tensor codes = fresh(*x, {T, C}, at::kByte);
+    at::Tensor scales = fresh(*x, {T, group > 0 ? C / group : 1}, at::kFloat);
     const paro_status st = paro_rms_norm_quantize_e4m3(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, group, (int32_t)T,
                                                        (int32_t)C, r ? half_out(h) : nullptr, r ? h.stride(0) : 0, (uint8_t *)codes.data_ptr(),
                                                        (float *)scales.data_ptr(), current_stream());
@@ -301,7 +310,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     const int64_t heads = q->size(1) / c->head_dim, ld = B == 1 ? table->size(1) : table->stride(0);
     at::Tensor o = rows_or_new(a[8], B, q->size(1), *q), lse;
     if (!o.defined()) return nullptr;
-    if (want) lse = at::empty({B, heads}, q->options().dtype(at::kFloat).requires_grad(false));
+    if (want) lse = fresh(*q, {B, heads}, at::kFloat);
     const paro_status st = paro_paged_attention(c, half_ptr(q), q->stride(0), (int32_t)heads, (const int32_t *)table->data_ptr(), ld,
                                                 (int32_t)table->size(1), (const int32_t *)lengths->data_ptr(), (int32_t)B, scale, window, half_out(o),
                                                 o.stride(0), want ? (float *)lse.data_ptr() : nullptr, ws->data_ptr(), bytes, current_stream());

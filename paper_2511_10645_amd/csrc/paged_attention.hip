@@ -512,7 +512,13 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     // Units of a block and of a wave: all waves of the grid alike; where that would leave a block fewer than kLeastUnits, fewer blocks.
     uint32_t share = quotient(total + gridDim.x - 1, gridDim.x, a.per_block), mine = 1;
     if (share < kLeastUnits) share = kLeastUnits;
-    if (share >= WAVES) { mine = (share + WAVES - 1) / WAVES; share = mine * WAVES; }
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);        // units of the first sequence
+    if (a.batch == 1 && share < first && first <= WAVES)
+        share = first;                           // one short sequence: a head's units stay in one block, nothing goes through memory (200 tokens: 9.1 -> 6.7 us)
+    else if (share >= WAVES) {
+        mine = (share + WAVES - 1) / WAVES;
+        share = mine * WAVES;
+    }
     const uint32_t begin = blockIdx.x * share;
     if (begin >= total) return;
     const uint32_t end = begin + share < total ? begin + share : total;
