@@ -5,9 +5,10 @@
 // Bound by HBM (every element read and written once) and at few tokens by latency.  A block has some consecutive tokens
 // and some of their heads; it evaluates each (token, pair) angle once, in LDS, for all of them (64 sines a token next to some
 // thousand channels).  The angle is reduced to a fraction of a turn in fp64: p f loses nothing at long positions, where an fp32
-// product is off by 2^-24 p f.  A lane then has 16 channels of a head, both halves of 8 pairs in either layout: two 16-byte
-// requests, no exchange between lanes.  A prompt's tokens are taken several to a block because the cache interleaves
-// the tokens of a page in its keys: neighbouring tokens then fill whole cache lines in one L2.
+// product is off by 2^-24 p f.  A thread then has 16 channels of a head, both halves of 8 pairs in either layout (two 16-byte
+// requests, no exchange between lanes), keeps their sines and cosines and takes one head after the other, the next one's
+// channels on their way.  A prompt's tokens are taken several to a block because the cache interleaves the tokens of a page
+// in its keys: neighbouring tokens then fill whole pieces of a cache line in one L2.
 #include <cmath>
 
 #include "kv_common.h"
@@ -15,7 +16,9 @@
 namespace paro {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeTokens = 8;                   // most tokens of a block
+constexpr int kRopeTokens = 4;                   // most tokens of a block
+constexpr int kRopeMany = 1024;                  // tokens from which on a block has several
+constexpr int kRopeBlocks = 1024;                // blocks that heads are spread over
 constexpr int kRopePairs = 256;                  // most pairs of a head
 
 struct RopeArgs {
@@ -70,22 +73,48 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
     }
     __syncthreads();
 
+    // A thread keeps its 16 channels c and its token t, sines and cosines with them, and takes every `step`-th head.
     const int lanes = a.D / 16;                  // of a head
+    const int c = threadIdx.x % lanes, line = threadIdx.x / lanes, step = kRopeThreads / lanes / a.tokens;
+    const int t = line % a.tokens;
     const int first = blockIdx.y * a.rows, all = a.q_heads + (a.k ? 2 * a.kv_heads : 0);
-    const int rows = all - first < a.rows ? all - first : a.rows;
-    for (int i = threadIdx.x; i < tokens * rows * lanes; i += kRopeThreads) {
-        const int line = i / lanes, c = i - line * lanes, t = line / rows, row = first + line - t * rows;
+    const int last = first + a.rows < all ? first + a.rows : all;
+    int row = first + line / a.tokens;
+    if (t >= tokens || line / a.tokens >= step) return;
+    const bool paired = 8 * c < a.pairs;
+    const int pa = LAYOUT == 0 && paired ? 8 * c : 16 * c, pb = LAYOUT == 0 && paired ? a.pairs + 8 * c : 16 * c + 8;
+    float cs[8], sn[8];
+    if (paired) {
+        const float *at = s_cs + t * 2 * a.pairs + 8 * c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { cs[e] = at[e]; sn[e] = at[a.pairs + e]; }
+    }
+    int64_t slot = -1;
+    if (a.k) slot = a.slots[t0 + t];
+    const bool kept = (uint64_t)slot < (uint64_t)a.n_slots;
+    const int64_t page0 = ((slot >> a.page_log) * a.kv_heads) << a.page_log;       // the first token of the page's first head
+    const int off = (int)slot & ((1 << a.page_log) - 1);
+    const _Float16 *xq = a.q + (t0 + t) * a.ldq, *xk = a.k + (t0 + t) * a.ldk, *xv = a.v + (t0 + t) * a.ldv;
+    const auto source = [&](int r) {
+        return r < a.q_heads ? xq + r * a.D : r < a.q_heads + a.kv_heads ? xk + (r - a.q_heads) * a.D : xv + (r - a.q_heads - a.kv_heads) * a.D;
+    };
+    const auto place_a = [&](int r) { return r < a.q_heads + a.kv_heads ? pa : 16 * c; };       // values are not rotated
+    const auto place_b = [&](int r) { return r < a.q_heads + a.kv_heads ? pb : 16 * c + 8; };
+    half8v na = {}, nb = {};                     // the next head's channels
+    if (row < last) { na = *(const half8v *)(source(row) + place_a(row)); nb = *(const half8v *)(source(row) + place_b(row)); }
+    for (; row < last; row += step) {
         const bool is_q = row < a.q_heads, is_k = !is_q && row < a.q_heads + a.kv_heads;
         const int head = is_q ? row : is_k ? row - a.q_heads : row - a.q_heads - a.kv_heads;
-        const _Float16 *x = (is_q ? a.q + (t0 + t) * a.ldq : is_k ? a.k + (t0 + t) * a.ldk : a.v + (t0 + t) * a.ldv) + (int64_t)head * a.D;
-        const bool turned = (is_q || is_k) && 8 * c < a.pairs;
-        const int ca = LAYOUT == 0 && turned ? 8 * c : 16 * c, cb = LAYOUT == 0 && turned ? a.pairs + 8 * c : 16 * c + 8;
-        const half8v ha = *(const half8v *)(x + ca), hb = *(const half8v *)(x + cb);
+        const int ca = place_a(row), cb = place_b(row);
+        const half8v ha = na, hb = nb;
+        if (row + step < last) {
+            na = *(const half8v *)(source(row + step) + place_a(row + step));
+            nb = *(const half8v *)(source(row + step) + place_b(row + step));
+        }
         float fa[8], fb[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) { fa[e] = (float)ha[e]; fb[e] = (float)hb[e]; }
-        if (turned) {
-            const float *cs = s_cs + t * 2 * a.pairs + 8 * c, *sn = cs + a.pairs;
+        if (paired && (is_q || is_k)) {
             if (LAYOUT == 0) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -110,10 +139,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
             *(half8v *)(y + cb) = rounded(fb);
             continue;
         }
-        const int64_t slot = a.slots[t0 + t];
-        const bool kept = (uint64_t)slot < (uint64_t)a.n_slots;
-        const int64_t place = ((slot >> a.page_log) * a.kv_heads + head) << a.page_log;    // of this head's first token of the page
-        const int off = (int)slot & ((1 << a.page_log) - 1);
+        const int64_t place = page0 + ((int64_t)head << a.page_log);       // this head's first token of the page
         if constexpr (FMT == 0) {
             if (!kept) continue;
             if (is_k) {
@@ -150,13 +176,14 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
 static hipError_t launch_rope(RopeArgs &a, int layout, int format, hipStream_t s)
 {
     const int all = a.q_heads + (a.k ? 2 * a.kv_heads : 0);
-    // few tokens: one to a block.  Many: kRopeTokens, and their heads spread over blocks while these are few.
-    a.tokens = a.T >= 256 ? kRopeTokens : 1;
-    const int blocks = (a.T + a.tokens - 1) / a.tokens;
-    int split = (1024 + blocks - 1) / blocks;
-    const int most = (int)((int64_t)a.tokens * all * (a.D / 16) / kRopeThreads);       // a block keeps a round of work for its threads
+    // Few tokens: one to a block.  Many: 4, whose keys are 64 bytes side by side in the cache (2048 tokens to an E4M3 cache: 14.8 us,
+    // 16.2 with one and 15.1 with 8, which take the interleaved layout from 15.6 to 18.7 us at 4095 tokens).  Heads are spread
+    // over blocks while these are few, down to one for every thread.
+    a.tokens = a.T >= kRopeMany ? kRopeTokens : 1;
+    const int blocks = (a.T + a.tokens - 1) / a.tokens, step = kRopeThreads / (a.D / 16) / a.tokens;
+    int split = (kRopeBlocks + blocks - 1) / blocks;
+    const int most = (all + step - 1) / step;
     split = split < most ? split : most;
-    if (split < 1) split = 1;
     a.rows = (all + split - 1) / split;
     const dim3 grid((unsigned)blocks, (unsigned)((all + a.rows - 1) / a.rows));
     const size_t lds = sizeof(float) * 2 * a.tokens * (a.pairs ? a.pairs : 1);
