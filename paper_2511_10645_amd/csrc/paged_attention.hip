@@ -22,6 +22,7 @@
 // the matrix cores have nothing else to do), after a factor of 2^15 (the largest p is 2^15, so that 11 bits are kept
 // down to 2^-29 of it); sums stay in fp32.
 #include <cmath>
+#include <type_traits>
 
 #include "kv_common.h"
 
@@ -430,24 +431,35 @@ template <int D, int THREADS>
 __device__ inline Four join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Segment &g, uint32_t share, uint32_t first, uint32_t step, uint32_t last,
                                   int item0, int items, int tid)
 {
-    // `lots` groups of threads take every lots-th part
-    constexpr int kLots = 4, kBatch = 4;
-    int lots = THREADS / items;
-    lots = lots < kLots ? lots : kLots;
-    const int lot = tid / items, i = item0 + tid - lot * items, query = i / (D / 4), channel = (i % (D / 4)) * 4;
+    constexpr int kLots = 4;
     Four x;
     x.clear();
-    if (lot < lots)
-        for (uint32_t j = first + lot * step; j <= last; j += kBatch * lots * step)
-            x.add<kBatch>([&](int z, float &m, float &l, F4 &v) {
-                const uint32_t k = j + z * lots * step;
-                // past the last one: a request beyond the buffer, which gives zeros
-                const uint32_t row = k <= last ? ((2 * k + (g.seg0 >= k * share)) * part_floats<D>() + query * (D + 4)) * 4u : 0x80000000u;
-                const U2 ml = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, row, 0, kAgent));
-                v = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
-                m = k <= last ? __uint_as_float(ml[0]) : -INFINITY;
-                l = __uint_as_float(ml[1]);
-            });
+    // parts k0, k0 + by, ..., N of them or as many as there are, for item i
+    const auto take = [&](auto n, uint32_t k0, uint32_t by, int i) {
+        const int query = i / (D / 4), channel = (i % (D / 4)) * 4;
+        x.add<decltype(n)::value>([&](int z, float &m, float &l, F4 &v) {
+            const uint32_t k = k0 + z * by;
+            // past the last one: a request beyond the buffer, which gives zeros
+            const uint32_t row = k <= last ? ((2 * k + (g.seg0 >= k * share)) * part_floats<D>() + query * (D + 4)) * 4u : 0x80000000u;
+            const U2 ml = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, row, 0, kAgent));
+            v = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(r, row + (4 + channel) * 4u, 0, kAgent));
+            m = k <= last ? __uint_as_float(ml[0]) : -INFINITY;
+            l = __uint_as_float(ml[1]);
+        });
+    };
+    // Few parts: every thread reads all of its item.  More: `lots` groups of threads take every lots-th part and meet in LDS.
+    int lots = 1;
+    if (last - first < 4 * step) {
+        if (tid < items) take(std::integral_constant<int, 4>(), first, step, item0 + tid);
+    } else if (last - first < 8 * step) {
+        if (tid < items) take(std::integral_constant<int, 8>(), first, step, item0 + tid);
+    } else {
+        lots = THREADS / items;
+        lots = lots < kLots ? lots : kLots;
+        const int lot = tid / items;
+        if (lot < lots)
+            for (uint32_t j = first + lot * step; j <= last; j += 4 * lots * step) take(std::integral_constant<int, 4>(), j, lots * step, item0 + tid - lot * items);
+    }
     if (lots > 1) {
         F4 *sv = (F4 *)s;
         U2 *sm = (U2 *)(s + 4 * THREADS);
