@@ -350,18 +350,17 @@ struct Segment {
 };
 struct Target {
     int head, first, queries;                    // key-value head, first query head, their number
-    int64_t o, lse;
     Target() = default;
-    __device__ Target(const AttnArgs &a, int b, int seg, int D)
+    __device__ Target(const AttnArgs &a, int seg)
     {
         int chunk = 0;
         head = seg;
         if (a.chunks > 1) { head = seg / a.chunks; chunk = seg - head * a.chunks; }
         first = head * a.group + chunk * kQueries;
         queries = a.group - chunk * kQueries < kQueries ? a.group - chunk * kQueries : kQueries;
-        o = (int64_t)b * a.ldo + (int64_t)first * D;
-        lse = (int64_t)b * (a.kv_heads * a.group) + first;
     }
+    __device__ _Float16 *o(const AttnArgs &a, int b, int D) const { return a.o + (int64_t)b * a.ldo + (int64_t)first * D; }
+    __device__ float *lse(const AttnArgs &a, int b) const { return a.lse + (int64_t)b * (a.kv_heads * a.group) + first; }
 };
 
 // The blocks that share a segment, and the group of them that block `me` is in.
@@ -405,11 +404,11 @@ struct Four {
         }
         m = top;
     }
-    __device__ void result(const AttnArgs &a, const Target &to, int D, int query, int channel) const
+    __device__ void result(const AttnArgs &a, const Target &to, int b, int D, int query, int channel) const
     {
         const float inv = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-        *(half4v *)(a.o + to.o + query * D + channel) = half4v{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
-        if (a.lse && channel == 0) a.lse[to.lse + query] = lse_of(m, l);
+        *(half4v *)(to.o(a, b, D) + query * D + channel) = half4v{(_Float16)(v[0] * inv), (_Float16)(v[1] * inv), (_Float16)(v[2] * inv), (_Float16)(v[3] * inv)};
+        if (a.lse && channel == 0) to.lse(a, b)[query] = lse_of(m, l);
     }
 };
 
@@ -458,7 +457,7 @@ __device__ inline Four join_parts(__amdgpu_buffer_rsrc_t r, float *s, const Segm
         lots = lots < kLots ? lots : kLots;
         const int lot = tid / items;
         if (lot < lots)
-            for (uint32_t j = first + lot * step; j <= last; j += 4 * lots * step) take(std::integral_constant<int, 4>(), j, lots * step, item0 + tid - lot * items);
+            for (uint32_t j = first + lot * step; j <= last; j += 8 * lots * step) take(std::integral_constant<int, 8>(), j, lots * step, item0 + tid - lot * items);
     }
     if (lots > 1) {
         F4 *sv = (F4 *)s;
@@ -576,7 +575,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         u0 = pl.sp.unit0 + (int)(at - g.seg0);
         u1 = pl.sp.unit0 + (int)((g.seg1 < wend ? g.seg1 : wend) - g.seg0);
         turn(u0);
-        to = Target(a, g.b, g.seg, D);
+        to = Target(a, g.seg);
         h.head = to.head;
         h.at = (int64_t)h.bytes * h.head;
         const _Float16 *qp = a.q + (int64_t)g.b * a.ldq + (int64_t)(to.first + (n < to.queries ? n : 0)) * D;
@@ -621,7 +620,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
             if (at == g.seg0 && stop == g.seg1) {        // all of the segment is here
                 if (n < to.queries) {
                     const float inv = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-                    _Float16 *o = a.o + to.o + (int64_t)n * D + quarter * 4 * R;
+                    _Float16 *o = to.o(a, g.b, D) + n * D + quarter * 4 * R;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if constexpr (R == 4) {
@@ -637,7 +636,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                             }
                         }
                     }
-                    if (a.lse && quarter == 0) a.lse[to.lse + n] = lse_of(st.m, l);
+                    if (a.lse && quarter == 0) to.lse(a, g.b)[n] = lse_of(st.m, l);
                 }
             } else {
                 const int slot = 2 * wave + (g.seg0 >= wbegin);          // the segment that goes on from before, or the one that goes on after
@@ -674,7 +673,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         const Segment g = held.of_lane(slot0);
         const uint32_t behind = (uint32_t)__ballot(there && !(lane & 1) && lane > slot0 && held.seg0 == g.seg0);
         const int links = 1 + __builtin_popcount(behind);
-        const Target to(a, g.b, g.seg, D);
+        const Target to(a, g.seg);
         const bool whole = g.seg0 >= begin && g.seg1 <= end;
         for (int i = tid - team * team_waves * 64; i < to.queries * (D / 4); i += team_waves * 64 < THREADS ? team_waves * 64 : THREADS) {
             const int query = i / (D / 4), channel = (i % (D / 4)) * 4;
@@ -690,7 +689,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                     l = s_l[slot * kQueries + query];
                     v = *(const F4 *)(s_o + (slot * rows + query) * kRow + channel);
                 });
-            if (whole) x.result(a, to, D, query, channel);
+            if (whole) x.result(a, to, g.b, D, query, channel);
             else store_part<D>(parts, 2 * blockIdx.x + (g.seg0 >= begin), query, channel, x);
         }
     }
@@ -714,7 +713,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     for (int z = 0; z < 2; ++z) {
         if (!__builtin_amdgcn_readfirstlane(s_last[z])) continue;
         const Segment g = z == 0 ? from : on;
-        const Target to(a, g.b, g.seg, D);
+        const Target to(a, g.seg);
         const Sharers by(g, share, per_share, blockIdx.x);
         const int items = to.queries * (D / 4);
         bool final = !by.in_groups;
@@ -734,7 +733,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
             for (int i0 = 0; i0 < items; i0 += THREADS) {
                 const int some = items - i0 < THREADS ? items - i0 : THREADS;
                 const Four x = join_parts<D, THREADS>(parts, s_o, g, share, by.first, by.in_groups ? kGroupParts : 1, by.last, i0, some, tid);
-                if (tid < some) x.result(a, to, D, (i0 + tid) / (D / 4), ((i0 + tid) % (D / 4)) * 4);
+                if (tid < some) x.result(a, to, g.b, D, (i0 + tid) / (D / 4), ((i0 + tid) % (D / 4)) * 4);
             }
     }
 }
