@@ -338,8 +338,8 @@ paro_status paro_rotated_linear_mxfp4(const paro_rotation *rot, const paro_mxfp4
 /* Root-mean-square norm with the residual's addition:
  *      h = X + R (R NULL: h = X),   Y[t][c] = h[t][c] / sqrt(mean_c h[t][c]^2 + eps) * weight[c]
  * The norm is taken of the unrounded fp32 h.  H (NULL: not wanted) receives h rounded to fp16.
- * C a multiple of 8, at most 32768; weight: [C] fp16, 16-byte aligned.  H and Y may each be X or R
- * itself (same row stride); H and Y must differ.  No workspace. */
+ * C a multiple of 8, at most 32768; T at most 2^21; weight: [C] fp16, 16-byte aligned.  H and Y may each be X or R
+ * itself (same row stride); H and Y must differ.  eps finite, >= 0 (with 0 a row of zeros gives NaN).  No workspace. */
 paro_status paro_rms_norm(const paro_half_t *X, int64_t ldx, const paro_half_t *R, int64_t ldr,
                           const paro_half_t *weight, float eps, int32_t T, int32_t C, paro_half_t *H,
                           int64_t ldh, paro_half_t *Y, int64_t ldy, void *stream);
@@ -383,7 +383,7 @@ paro_status paro_rope_frequencies_host(int32_t rot_dim, double base, int32_t sca
                                        float *magnitude_host);
 
 /* Y[t] = the T rows of X with every head's channels rotated; heads * rope->head_dim channels a row.
- * positions: device [T].  Y == X (same ld) is allowed.  No workspace. */
+ * positions: device [T], T at most 2^24.  Y == X (same ld) is allowed.  No workspace. */
 paro_status paro_rope(const paro_rope_t *rope, const paro_half_t *X, int64_t ldx, const int32_t *positions,
                       int32_t heads, int32_t T, paro_half_t *Y, int64_t ldy, void *stream);
 
@@ -393,7 +393,8 @@ paro_status paro_rope(const paro_rope_t *rope, const paro_half_t *X, int64_t ldx
  *   format 0: fp16, k [n_pages][kv_heads][head_dim/8][page][8], v [n_pages][kv_heads][page][head_dim]
  *   format 1: E4M3 codes, k [n_pages][kv_heads][head_dim/16][page][16], v [n_pages][kv_heads][page][head_dim],
  *             and one scale byte per token and head, k_scale / v_scale [n_pages][kv_heads][page]: the code's
- *             value counts 2^(byte - 127) times */
+ *             value counts 2^(byte - 127) times.  paro_kv_append writes bytes 112 to 135; with those of a caller's
+ *             own outside, values that fp16 does not have are rounded or infinite */
 typedef struct {
     int32_t n_pages;
     int32_t page;             /* tokens of a page: a power of two, 16..1024                     */
@@ -405,7 +406,7 @@ typedef struct {
 } paro_kv_cache;
 
 /* The keys and values of T new tokens into their slots, and on the way the rotation of keys and queries.
- * K, V: fp16 rows of kv_heads heads; slots: device [T], a negative slot, or one the cache does not have,
+ * K, V: fp16 rows of kv_heads heads, T at most 2^24; slots: device [T], a negative slot, or one the cache does not have,
  * leaves its token out of the cache (padding).  Slots of one call must differ.
  * rope: NULL leaves queries and keys as they are (positions may be NULL then); rope->head_dim must be the
  * cache's.  Q (NULL: none): rows of q_heads heads, rotated into Qr (Qr == Q, same ld, is allowed).
@@ -426,7 +427,9 @@ paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rope_t *rope, 
  * attend to (n <= 0, or every score -inf) gives zeros and lse -inf; n beyond the table is taken as the
  * table's end; tokens of a page the cache does not have are left out.  Cache places past n do not matter,
  * whatever they hold.  lse (NULL: not wanted): fp32 [batch][q_heads], ln sum_t exp(scale q . k_t).
- * Q, O: fp16 rows of q_heads heads of head_dim; q_heads a multiple of kv_heads.  scale must be finite.
+ * Q, O: fp16 rows of q_heads heads of head_dim; q_heads a multiple of kv_heads (16 of them share one reading of their
+ * key-value head).  scale must be finite.  A key or value that is not finite makes its heads' results not finite, unless
+ * its score is -inf.  table_width * page at most 2^30, as are the units of 32 tokens of all heads.
  * ws: >= paro_workspace_bytes_attention() bytes, 256-byte aligned, in the two parts described at
  * paro_workspace_bytes(): the exchange part (paro_workspace_exchange_bytes_attention(), zero-filled once,
  * all zero again after every call) counts arrivals, the scratch part at the buffer's end holds fp32 partial

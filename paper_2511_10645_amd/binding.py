@@ -188,6 +188,7 @@ class _CtypesCalls:
         _gpu_vector(w, torch.float16, C)
         ldr = 0 if R is None else _gpu_rows(R, T, C)
         H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
+        _number(group)
         codes = torch.empty((T, C), dtype=torch.uint8, device=X.device)
         scales = torch.empty((T, C // group if group > 0 else 1), dtype=torch.float32, device=X.device)
         st = lib().paro_rms_norm_quantize_e4m3(X.data_ptr(), ldx, _ptr(R), ldr, w.data_ptr(), eps, group, T, C, _ptr(H), ldh, codes.data_ptr(),
@@ -232,7 +233,8 @@ class _CtypesCalls:
         assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
         assert table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.shape[0] == B and table.is_cuda
         _gpu_vector(lengths, torch.int32, B)
-        assert buf.is_cuda
+        assert buf.is_cuda and table.shape[1] < 2 ** 31
+        _number(window)
         heads = Q.shape[1] // cache.head_dim
         O, ldo = _rows_or_new(O, B, Q.shape[1], Q)
         lse = torch.empty((B, heads), dtype=torch.float32, device=Q.device) if with_lse else None
@@ -488,6 +490,7 @@ def _gpu_rows(x: torch.Tensor, T: int = -1, width: int | None = None) -> int:
     """The row stride of fp16 rows on the GPU, checked as the native calls check them."""
     rows, ld = _rows(x)
     assert x.is_cuda, "expected a tensor on the GPU"
+    assert rows < 2 ** 31, "more rows than 32 bits count"
     assert (T < 0 or rows == T) and (width is None or x.shape[1] == width), "tensors of different shapes"
     return ld
 
@@ -495,6 +498,10 @@ def _gpu_rows(x: torch.Tensor, T: int = -1, width: int | None = None) -> int:
 def _gpu_vector(x: torch.Tensor, dtype, n: int) -> None:
     assert x.dtype == dtype and x.dim() == 1 and x.is_contiguous() and x.shape[0] == n, "expected a contiguous vector of another type or length"
     assert x.is_cuda, "expected a tensor on the GPU"
+
+
+def _number(n: int) -> None:
+    assert -2 ** 31 <= n < 2 ** 31, "a number beyond 32 bits"
 
 
 def _rows_or_new(x, T: int, width: int, like: torch.Tensor):

@@ -142,6 +142,7 @@ bool gpu_rows(const at::Tensor &x, int64_t t, int64_t width)
 {
     if (!rows(x)) return false;
     if (!x.is_cuda()) return refuse("expected a tensor on the GPU");
+    if (x.size(0) > INT32_MAX) return refuse("more rows than 32 bits count");
     if ((t >= 0 && x.size(0) != t) || x.size(1) != width) return refuse("tensors of different shapes");
     return true;
 }
@@ -149,6 +150,14 @@ bool gpu_vector(const at::Tensor &x, at::ScalarType type, int64_t n)
 {
     if (x.scalar_type() != type || x.dim() != 1 || !x.is_contiguous() || x.size(0) != n) return refuse("expected a contiguous vector of another type or length");
     return x.is_cuda() || refuse("expected a tensor on the GPU");
+}
+// A number of 32 bits; false with an exception set if it is none.
+bool number(PyObject *o, int32_t &to)
+{
+    const long long x = PyLong_AsLongLong(o);
+    if (x == -1 && PyErr_Occurred()) return false;
+    to = (int32_t)x;
+    return to == x || refuse("a number beyond 32 bits");
 }
 // An optional tensor argument; false with an exception set if it is anything else.
 bool maybe(PyObject *o, const at::Tensor *&t)
@@ -220,9 +229,9 @@ PyObject *rms_norm_quantize_e4m3(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor *x = tensor(a[0]), *w = x ? tensor(a[1]) : nullptr, *r;
     if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*w, at::kHalf, x->size(1))) return nullptr;
     const float eps = (float)PyFloat_AsDouble(a[2]);
-    const int32_t group = (int32_t)PyLong_AsLong(a[3]);
+    int32_t group;
     const int64_t T = x->size(0), C = x->size(1);
-    if (PyErr_Occurred() || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    if (PyErr_Occurred() || !number(a[3], group) || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
     at::Tensor h;
     if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
     at::Tensor codes = fresh(*x, {T, C}, at::kByte);
@@ -304,9 +313,10 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!ws->is_cuda()) { refuse("expected a tensor on the GPU"); return nullptr; }
     const size_t bytes = PyLong_AsSize_t(a[5]);
     const float scale = (float)PyFloat_AsDouble(a[6]);
-    const int32_t window = (int32_t)PyLong_AsLong(a[7]);
+    int32_t window;
     const int want = PyObject_IsTrue(a[9]);
-    if (PyErr_Occurred() || want < 0) return nullptr;
+    if (PyErr_Occurred() || want < 0 || !number(a[7], window)) return nullptr;
+    if (table->size(1) > INT32_MAX) { refuse("more pages than 32 bits count"); return nullptr; }
     const int64_t heads = q->size(1) / c->head_dim, ld = B == 1 ? table->size(1) : table->stride(0);
     at::Tensor o = rows_or_new(a[8], B, q->size(1), *q), lse;
     if (!o.defined()) return nullptr;

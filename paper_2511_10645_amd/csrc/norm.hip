@@ -23,6 +23,7 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 256;
+constexpr int kNormRows = 1 << 21;               // a launch holds fewer than 2^32 threads, up to 1024 of them for a row
 
 enum NormOut { kNormF16, kNormRow, kNormGroup };
 
@@ -129,7 +130,7 @@ template <int LANES, int NV, NormOut OUT>
 static hipError_t launch_norm_as(const NormArgs &a, hipStream_t s)
 {
     constexpr int kThreads = LANES < kNormThreads ? kNormThreads : LANES, kRows = kThreads / LANES;
-    hipLaunchKernelGGL((norm_kernel<LANES, NV, OUT>), dim3((unsigned)((a.T + kRows - 1) / kRows)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((norm_kernel<LANES, NV, OUT>), dim3(((unsigned)a.T + kRows - 1) / kRows), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
@@ -152,7 +153,7 @@ static paro_status norm_checks(const paro_half_t *X, int64_t ldx, const paro_hal
     if (!X || !weight) return PARO_ERR_NULL;
     if (T <= 0 || C <= 0 || !(eps >= 0.0f) || !std::isfinite(eps)) return PARO_ERR_SHAPE;
     if (C % 8) return PARO_ERR_ALIGN;
-    if (C > 32768) return PARO_ERR_UNSUPPORTED;
+    if (C > 32768 || T > kNormRows) return PARO_ERR_UNSUPPORTED;
     if (const paro_status st = check_rows(X, ldx, C); st != PARO_OK) return st;
     if (R) if (const paro_status st = check_rows(R, ldr, C); st != PARO_OK) return st;
     if (H) if (const paro_status st = check_rows(H, ldh, C); st != PARO_OK) return st;

@@ -791,7 +791,7 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     const paro_kv_cache &c = *cache;
     if (batch <= 0 || q_heads <= 0 || q_heads % c.kv_heads || table_width <= 0 || window < 0) return PARO_ERR_SHAPE;
     if (ld_table != 0 && ld_table < table_width) return PARO_ERR_SHAPE;
-    if (!std::isfinite(scale)) return PARO_ERR_SHAPE;
+    if (!std::isfinite(scale * kLog2e)) return PARO_ERR_SHAPE;
     if (const paro_status st = check_rows(Q, ldq, (int64_t)q_heads * c.head_dim); st != PARO_OK) return st;
     if (const paro_status st = check_rows(O, ldo, (int64_t)q_heads * c.head_dim); st != PARO_OK) return st;
     if (!aligned(block_table, 4) || !aligned(lengths, 4) || (lse && !aligned(lse, 4))) return PARO_ERR_ALIGN;

@@ -19,6 +19,7 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 4;                   // most tokens of a block
 constexpr int kRopeMany = 1024;                  // tokens from which on a block has several
 constexpr int kRopeBlocks = 1024;                // blocks that heads are spread over
+constexpr int kRopeMost = 1 << 24;               // tokens of a call: a launch holds fewer than 2^32 threads
 constexpr int kRopePairs = 256;                  // most pairs of a head
 
 struct RopeArgs {
@@ -219,7 +220,7 @@ extern "C" paro_status paro_rope(const paro_rope_t *rope, const paro_half_t *X, 
     if (const paro_status st = check_rows(Y, ldy, (int64_t)heads * rope->head_dim); st != PARO_OK) return st;
     if (X == Y && ldx != ldy) return PARO_ERR_SHAPE;
     if (!aligned(positions, 4)) return PARO_ERR_ALIGN;
-    if (heads > 65535) return PARO_ERR_UNSUPPORTED;
+    if (heads > 65535 || T > kRopeMost) return PARO_ERR_UNSUPPORTED;
     RopeArgs a = {};
     a.q = (const _Float16 *)X; a.ldq = ldx; a.qr = (_Float16 *)Y; a.ldqr = ldy;
     a.inv_freq = rope->inv_freq; a.positions = positions; a.magnitude = rope->magnitude;
@@ -249,7 +250,7 @@ extern "C" paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rop
         if (Q == Qr && ldq != ldqr) return PARO_ERR_SHAPE;
     }
     if (!aligned(slots, 8) || (positions && !aligned(positions, 4))) return PARO_ERR_ALIGN;
-    if (c.kv_heads > 65535 || (Q && q_heads > 65535)) return PARO_ERR_UNSUPPORTED;
+    if (c.kv_heads > 65535 || (Q && q_heads > 65535) || T > kRopeMost) return PARO_ERR_UNSUPPORTED;
     RopeArgs a = {};
     a.q = (const _Float16 *)Q; a.ldq = ldq; a.qr = (_Float16 *)Qr; a.ldqr = ldqr; a.q_heads = Q ? q_heads : 0;
     a.k = (const _Float16 *)K; a.ldk = ldk; a.v = (const _Float16 *)V; a.ldv = ldv; a.kv_heads = c.kv_heads;

@@ -32,7 +32,7 @@ def test_norm_refusals():
     assert f(eps=-1.0) == E_SHAPE and f(eps=math.nan) == E_SHAPE and f(eps=math.inf) == E_SHAPE
     assert f(C=252) == E_ALIGN and f(X=FAKE + 2) == E_ALIGN and f(ldx=260) == E_ALIGN and f(w=FAKE + 8) == E_ALIGN
     assert f(R=FAKE, ldr=8) == E_SHAPE and f(R=FAKE + 8, ldr=256) == E_ALIGN and f(H=FAKE, ldh=128) == E_SHAPE
-    assert f(C=32776, ldx=32776, ldy=32776) == E_UNSUP
+    assert f(C=32776, ldx=32776, ldy=32776) == E_UNSUP and f(T=2 ** 21 + 1) == E_UNSUP and f(T=2 ** 31 - 1) == E_UNSUP
     assert f(H=FAKE * 2, ldh=256) == E_SHAPE                            # H and Y in one place
     assert f(Y=FAKE, ldy=512) == E_SHAPE and f(H=FAKE, ldh=512) == E_SHAPE        # in place with other strides
     assert q(codes=None) == E_NULL and q(scales=None) == E_NULL and q(group=64) == E_UNSUP and q(C=264, ldx=264) == E_SHAPE
@@ -46,7 +46,7 @@ def test_rope_and_append_refusals():
     assert f(T=0) == E_SHAPE and f(heads=0) == E_SHAPE and f(heads=3) == E_SHAPE and f(rp=_rope(rot_dim=144)) == E_SHAPE
     assert f(rp=_rope(magnitude=math.inf)) == E_SHAPE and f(Y=FAKE, ldy=264) == E_SHAPE
     assert f(rp=_rope(rot_dim=24)) == E_UNSUP and f(rp=_rope(layout=2)) == E_UNSUP and f(rp=_rope(head_dim=100, rot_dim=16)) == E_UNSUP
-    assert f(rp=_rope(head_dim=528, rot_dim=16)) == E_UNSUP
+    assert f(rp=_rope(head_dim=528, rot_dim=16)) == E_UNSUP and f(T=2 ** 31 - 1) == E_UNSUP
     assert f(X=FAKE + 2) == E_ALIGN and f(pos=FAKE + 2) == E_ALIGN and f(ldx=260) == E_ALIGN
     a = lambda c=_cache(), rp=_rope(), K=FAKE, ldk=256, V=FAKE, ldv=256, slots=FAKE, pos=FAKE, T=1, Q=FAKE, ldq=512, hq=4, Qr=FAKE * 2, ldqr=512: L.paro_kv_append(
         r(c) if c else None, r(rp) if rp else None, K, ldk, V, ldv, slots, pos, T, Q, ldq, hq, Qr, ldqr, None)
@@ -54,7 +54,7 @@ def test_rope_and_append_refusals():
     assert a(K=None) == E_NULL and a(V=None) == E_NULL and a(slots=None) == E_NULL and a(pos=None) == E_NULL and a(Qr=None) == E_NULL
     assert a(c=_cache(n_pages=0)) == E_SHAPE and a(c=_cache(kv_heads=0)) == E_SHAPE and a(T=0) == E_SHAPE and a(hq=0) == E_SHAPE
     assert a(c=_cache(page=8)) == E_UNSUP and a(c=_cache(page=24)) == E_UNSUP and a(c=_cache(page=2048)) == E_UNSUP and a(c=_cache(head_dim=96)) == E_UNSUP
-    assert a(c=_cache(format=2)) == E_UNSUP
+    assert a(c=_cache(format=2)) == E_UNSUP and a(T=2 ** 31 - 1) == E_UNSUP
     assert a(rp=_rope(head_dim=64, rot_dim=64)) == E_SHAPE and a(ldk=128) == E_SHAPE and a(ldv=128) == E_SHAPE and a(ldq=256) == E_SHAPE and a(ldqr=256) == E_SHAPE
     assert a(Q=FAKE, Qr=FAKE, ldqr=520) == E_SHAPE
     assert a(c=_cache(k=FAKE + 8)) == E_ALIGN and a(c=_cache(format=1, ks=FAKE + 1, vs=FAKE)) == E_ALIGN and a(slots=FAKE + 4) == E_ALIGN and a(pos=FAKE + 2) == E_ALIGN
@@ -68,6 +68,7 @@ def test_attention_refusals_and_workspace():
         L.paro_paged_attention(r(c) if c else None, Q, ldq, hq, table, ldt, width, lengths, batch, scale, window, O, ldo, lse, ws, n, None)
     assert f(c=None) == E_NULL and f(Q=None) == E_NULL and f(O=None) == E_NULL and f(table=None) == E_NULL and f(lengths=None) == E_NULL
     assert f(batch=0) == E_SHAPE and f(hq=7) == E_SHAPE and f(hq=0) == E_SHAPE and f(width=0) == E_SHAPE and f(window=-1) == E_SHAPE and f(ldt=3) == E_SHAPE
+    assert f(scale=3e38) == E_SHAPE                                     # finite, but not in units of log2
     assert f(scale=math.nan) == E_SHAPE and f(scale=math.inf) == E_SHAPE and f(ldq=512) == E_SHAPE and f(ldo=512) == E_SHAPE
     assert f(Q=FAKE + 2) == E_ALIGN and f(ldo=1028) == E_ALIGN and f(lse=FAKE + 2) == E_ALIGN and f(ws=FAKE + 128) == E_ALIGN and f(lengths=FAKE + 1) == E_ALIGN
     assert f(ws=None) == E_WS and f(n=need - 1) == E_WS
