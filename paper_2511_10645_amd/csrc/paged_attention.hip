@@ -102,28 +102,35 @@ __device__ inline Span span_of(const AttnArgs &a, int n)
     return s;
 }
 
-// Walks the segments: 64 sequences at a time, one to a lane.
+// Walks the sequences with their lengths in the lanes, 64 of them at a time.
 struct Place {
-    int chunk, length;                           // the lanes' sequences 64 chunk + lane, and their lengths
+    int first, length;                           // the lanes' sequences first + lane, and their lengths
     int b;                                       // current sequence, the number of its first unit and its span
     uint32_t base;
     Span sp;
-    __device__ void lanes(const AttnArgs &a, int c, int lane)
+    __device__ void lanes(const AttnArgs &a, int i, int lane)
     {
-        chunk = c;
-        const int i = 64 * c + lane;
-        length = a.lengths[i < a.batch ? i : a.batch - 1];
+        first = i;
+        length = a.lengths[i + lane < a.batch ? i + lane : a.batch - 1];
     }
     __device__ void sequence(const AttnArgs &a, int i, int lane)
     {
         b = i;
-        if (i >> 6 != chunk) lanes(a, i >> 6, lane);
-        sp = span_of(a, __builtin_amdgcn_readlane(length, i & 63));
+        if (i - first >= 64) lanes(a, i, lane);
+        sp = span_of(a, __builtin_amdgcn_readlane(length, i - first));
     }
     __device__ void next(const AttnArgs &a, int lane, uint32_t hc)
     {
         base += (uint32_t)sp.units * hc;
         sequence(a, b + 1, lane);
+    }
+    // Goes to the one of the lanes' sequences that holds unit `at`, given the sums of their units; false if it lies behind them.
+    __device__ bool find(const AttnArgs &a, uint32_t at, uint32_t upto, uint32_t hc, int lane)
+    {
+        const int before = __popcll(__ballot(base + upto * hc <= at));
+        if (before) base += (uint32_t)__builtin_amdgcn_readlane((int)upto, before - 1) * hc;
+        if (before < 64) sequence(a, first + before, lane);
+        return before < 64;
     }
 };
 
@@ -504,22 +511,24 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     const uint32_t hc = (uint32_t)(a.kv_heads * a.chunks);
     const int rows = a.group < kQueries ? a.group : kQueries;            // of a slot in LDS
 
-    // the units of all sequences, 64 sequences at a time; the first 64 stay
+    // the units of all sequences: lane i sums `per` consecutive ones
     Place pl;
-    const auto units_upto = [&](int c) {
-        pl.lanes(a, c, lane);
-        return sums_upto(64 * c + lane < a.batch ? (uint32_t)span_of(a, pl.length).units : 0u);
-    };
-    uint32_t total = 0;
-    for (int c = (a.batch - 1) >> 6; c > 0; --c) total += (uint32_t)__builtin_amdgcn_readlane((int)units_upto(c), 63);
-    uint32_t upto = units_upto(0);
-    total = (total + (uint32_t)__builtin_amdgcn_readlane((int)upto, 63)) * hc;
+    const int per = (a.batch + 63) >> 6;
+    uint32_t upto = 0;
+#pragma unroll 4
+    for (int j = 0; j < per; ++j) {
+        const int i = lane * per + j, n = a.lengths[i < a.batch ? i : a.batch - 1];
+        upto += i < a.batch ? (uint32_t)span_of(a, n).units : 0u;
+        pl.length = n;
+    }
+    upto = sums_upto(upto);
+    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
     // Units of a block and of a wave: all waves of the grid alike; where that would leave a block fewer than kLeastUnits, fewer blocks.
     uint32_t share = quotient(total + gridDim.x - 1, gridDim.x, a.per_block), mine = 1;
     if (share < kLeastUnits) share = kLeastUnits;
-    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);        // units of the first sequence
-    if (a.batch == 1 && share < first && first <= WAVES)
-        share = first;                           // one short sequence: a head's units stay in one block, nothing goes through memory (200 tokens: 9.1 -> 6.7 us)
+    const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);
+    if (a.batch == 1 && share < one && one <= WAVES)
+        share = one;                           // one short sequence: a head's units stay in one block, nothing goes through memory (200 tokens: 9.1 -> 6.7 us)
     else if (share >= WAVES) {
         mine = (share + WAVES - 1) / WAVES;
         share = mine * WAVES;
@@ -536,15 +545,16 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     const bool busy = wbegin < wend;
     if (busy) {
         pl.base = 0;
-        for (int c = 0;;) {                      // the sequence that holds unit wbegin
-            const int before = __popcll(__ballot(pl.base + upto * hc <= wbegin));
-            if (before < 64) {
-                if (before) pl.base += (uint32_t)__builtin_amdgcn_readlane((int)upto, before - 1) * hc;
-                pl.sequence(a, 64 * c + before, lane);
-                break;
+        pl.first = 0;
+        if (per == 1) {
+            pl.find(a, wbegin, upto, hc, lane);
+        } else {                                 // the lane whose sequences hold unit wbegin, and these one to a lane
+            const int before = __popcll(__ballot(upto * hc <= wbegin));
+            if (before) pl.base = (uint32_t)__builtin_amdgcn_readlane((int)upto, before - 1) * hc;
+            for (int i = before * per;; i += 64) {
+                pl.lanes(a, i, lane);
+                if (pl.find(a, wbegin, sums_upto(i + lane < a.batch ? (uint32_t)span_of(a, pl.length).units : 0u), hc, lane)) break;
             }
-            pl.base += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
-            upto = units_upto(++c);
         }
     }
     Head h;
