@@ -32,7 +32,7 @@ constexpr int kUnit = 32;                        // tokens of a unit
 constexpr int kAttnBlocks = 256;                 // most blocks of a launch: one for every compute unit
 constexpr int kQueries = 16;                     // query heads of a unit: the N of the matrix instruction
 constexpr uint32_t kLeastUnits = 4;              // of a block
-constexpr uint32_t kGroupParts = 32;                  // partial results that are joined at once
+constexpr uint32_t kGroupParts = 32;             // partial results that are joined at once
 constexpr float kPShift = 15.0f;                 // p is held 2^15 times
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRsrcRaw = 0x00020000;             // raw buffer, 32-bit data format
@@ -528,7 +528,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     if (share < kLeastUnits) share = kLeastUnits;
     const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);
     if (a.batch == 1 && share < one && one <= WAVES)
-        share = one;                           // one short sequence: a head's units stay in one block, nothing goes through memory (200 tokens: 9.1 -> 6.7 us)
+        share = one;                             // one short sequence: a head in one block, nothing goes through memory (200 tokens: 9.1 -> 6.7 us)
     else if (share >= WAVES) {
         mine = (share + WAVES - 1) / WAVES;
         share = mine * WAVES;
