@@ -42,7 +42,7 @@ def strided(x, more=24):
 
 # ---- norm ---------------------------------------------------------------------------------------------------------------
 
-NORM_SHAPES = [(1, 8), (3, 128), (17, 136), (5, 512), (2, 520), (1, 2048), (33, 2056), (7, 4096), (1, 5120), (3, 8192), (2, 14336), (1, 32768)]
+NORM_SHAPES = [(1, 8), (3, 128), (17, 136), (5, 512), (2, 520), (1, 2048), (33, 2056), (7, 4096), (1, 5120), (3, 776), (5, 1024), (3, 8192), (2, 14336), (1, 32768)]
 
 
 def _norm_inputs(T, C, seed):
@@ -70,7 +70,7 @@ def test_norm(P, T, C, residual):
 
 
 @pytest.mark.parametrize("T,C,group", [(1, 128, 128), (5, 128, 0), (3, 640, 128), (4, 1000, 0), (2, 2048, 128), (9, 4096, 128), (6, 5120, 0), (1, 8320, 128),
-                                       (2, 32768, 128), (2, 32768, 0)])
+                                       (2, 32768, 128), (2, 32768, 0), (5, 1024, 128), (5, 776, 0), (515, 4096, 128), (514, 2176, 0), (2, 7000, 0)])
 def test_norm_e4m3(P, T, C, group):
     say(f"norm e4m3 {T} x {C} group {group}")
     x, r, w = _norm_inputs(T, C, 7 * T + C)
