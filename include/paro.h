@@ -427,7 +427,7 @@ paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rope_t *rope, 
  * attend to (n <= 0, or every score -inf) gives zeros and lse -inf; n beyond the table is taken as the
  * table's end; tokens of a page the cache does not have are left out.  Cache places past n do not matter,
  * whatever they hold.  lse (NULL: not wanted): fp32 [batch][q_heads], ln sum_t exp(scale q . k_t).
- * Q, O: fp16 rows of q_heads heads of head_dim; q_heads a multiple of kv_heads (16 of them share one reading of their
+ * Q, O: fp16 rows of q_heads heads of head_dim, O nowhere in Q (PARO_ERR_SHAPE where O is Q); q_heads a multiple of kv_heads (16 of them share one reading of their
  * key-value head).  scale must be finite.  A key or value that is not finite makes its heads' results not finite, unless
  * its score is -inf.  table_width * page at most 2^30, as are the units of 32 tokens of all heads.
  * ws: >= paro_workspace_bytes_attention() bytes, 256-byte aligned, in the two parts described at

@@ -175,6 +175,7 @@ class _CtypesCalls:
         ldx = _gpu_rows(X)
         T, C = X.shape
         _gpu_vector(w, torch.float16, C)
+        assert R is not None or H is None, "H takes the sum with a residual"
         ldr = 0 if R is None else _gpu_rows(R, T, C)
         Y, ldy = _rows_or_new(Y, T, C, X)
         H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
@@ -186,6 +187,7 @@ class _CtypesCalls:
         ldx = _gpu_rows(X)
         T, C = X.shape
         _gpu_vector(w, torch.float16, C)
+        assert R is not None or H is None, "H takes the sum with a residual"
         ldr = 0 if R is None else _gpu_rows(R, T, C)
         H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
         _number(group)
@@ -214,14 +216,13 @@ class _CtypesCalls:
         _gpu_vector(slots, torch.int64, T)
         if positions is not None:
             _gpu_vector(positions, torch.int32, T)
+        assert Q is not None or Qr is None, "Qr takes rotated queries, and there are none"
         ldq = ldqr = heads = 0
         if Q is not None:
             ldq = _gpu_rows(Q, T)
             assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
             heads = Q.shape[1] // cache.head_dim
             Qr, ldqr = _rows_or_new(Qr, T, Q.shape[1], Q)
-        else:
-            Qr = None
         st = lib().paro_kv_append(ctypes.byref(cache), None if rope is None else ctypes.byref(rope), K.data_ptr(), ldk, V.data_ptr(), ldv,
                                   slots.data_ptr(), _ptr(positions), T, _ptr(Q), ldq, heads, _ptr(Qr), ldqr, _stream())
         return Qr if st == PARO_OK else st

@@ -210,11 +210,16 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     const float eps = (float)PyFloat_AsDouble(a[2]);
     const int64_t T = x->size(0), C = x->size(1);
     if (PyErr_Occurred() || !maybe(a[3], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    if (!r && a[5] != Py_None) { refuse("H takes the sum with a residual"); return nullptr; }
     at::Tensor y = rows_or_new(a[4], T, C, *x), h;
     if (!y.defined()) return nullptr;
     if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
-    const paro_status st = paro_rms_norm(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, (int32_t)T, (int32_t)C,
-                                         r ? half_out(h) : nullptr, r ? h.stride(0) : 0, half_out(y), y.stride(0), current_stream());
+    void *stream = current_stream();
+    paro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = paro_rms_norm(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, (int32_t)T, (int32_t)C,
+                       r ? half_out(h) : nullptr, r ? h.stride(0) : 0, half_out(y), y.stride(0), stream);
+    Py_END_ALLOW_THREADS
     if (st != PARO_OK) return PyLong_FromLong(st);
     PyObject *first = wrap(a[4], std::move(y));
     return r ? together({first, wrap(a[5], std::move(h))}) : first;
@@ -232,13 +237,18 @@ PyObject *rms_norm_quantize_e4m3(PyObject *, PyObject *const *a, Py_ssize_t n)
     int32_t group;
     const int64_t T = x->size(0), C = x->size(1);
     if (PyErr_Occurred() || !number(a[3], group) || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    if (!r && a[5] != Py_None) { refuse("H takes the sum with a residual"); return nullptr; }
     at::Tensor h;
     if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
     at::Tensor codes = fresh(*x, {T, C}, at::kByte);
     at::Tensor scales = fresh(*x, {T, group > 0 ? C / group : 1}, at::kFloat);
-    const paro_status st = paro_rms_norm_quantize_e4m3(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, group, (int32_t)T,
-                                                       (int32_t)C, r ? half_out(h) : nullptr, r ? h.stride(0) : 0, (uint8_t *)codes.data_ptr(),
-                                                       (float *)scales.data_ptr(), current_stream());
+    void *stream = current_stream();
+    paro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = paro_rms_norm_quantize_e4m3(half_ptr(x), x->stride(0), half_ptr(r), r ? r->stride(0) : 0, half_ptr(w), eps, group, (int32_t)T,
+                                     (int32_t)C, r ? half_out(h) : nullptr, r ? h.stride(0) : 0, (uint8_t *)codes.data_ptr(),
+                                     (float *)scales.data_ptr(), stream);
+    Py_END_ALLOW_THREADS
     if (st != PARO_OK) return PyLong_FromLong(st);
     PyObject *first = THPVariable_Wrap(std::move(codes)), *second = THPVariable_Wrap(std::move(scales));
     return r ? together({first, second, wrap(a[5], std::move(h))}) : together({first, second});
@@ -257,8 +267,12 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (rp->head_dim <= 0 || C % rp->head_dim) { refuse("rows are not whole heads"); return nullptr; }
     at::Tensor y = rows_or_new(a[3], T, C, *x);
     if (!y.defined()) return nullptr;
-    const paro_status st = paro_rope(rp, half_ptr(x), x->stride(0), (const int32_t *)at_->data_ptr(), (int32_t)(C / rp->head_dim), (int32_t)T,
-                                     half_out(y), y.stride(0), current_stream());
+    void *stream = current_stream();
+    paro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = paro_rope(rp, half_ptr(x), x->stride(0), (const int32_t *)at_->data_ptr(), (int32_t)(C / rp->head_dim), (int32_t)T,
+                   half_out(y), y.stride(0), stream);
+    Py_END_ALLOW_THREADS
     return st != PARO_OK ? PyLong_FromLong(st) : wrap(a[3], std::move(y));
     END_HANDLE_TH_ERRORS
 }
@@ -277,6 +291,7 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!rows(*k) || !gpu_rows(*k, -1, width) || !gpu_rows(*v, k->size(0), width)) return nullptr;
     const int64_t T = k->size(0);
     if (!gpu_vector(*slots, at::kLong, T) || (at_ && !gpu_vector(*at_, at::kInt, T))) return nullptr;
+    if (!q && a[7] != Py_None) { refuse("Qr takes rotated queries, and there are none"); return nullptr; }
     at::Tensor out;
     int64_t heads = 0;
     if (q) {
@@ -285,9 +300,13 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
         heads = q->size(1) / c->head_dim;
         if (!(out = rows_or_new(a[7], T, q->size(1), *q)).defined()) return nullptr;
     }
-    const paro_status st = paro_kv_append(c, rp, half_ptr(k), k->stride(0), half_ptr(v), v->stride(0), (const int64_t *)slots->data_ptr(),
-                                          at_ ? (const int32_t *)at_->data_ptr() : nullptr, (int32_t)T, half_ptr(q), q ? q->stride(0) : 0,
-                                          (int32_t)heads, q ? half_out(out) : nullptr, q ? out.stride(0) : 0, current_stream());
+    void *stream = current_stream();
+    paro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = paro_kv_append(c, rp, half_ptr(k), k->stride(0), half_ptr(v), v->stride(0), (const int64_t *)slots->data_ptr(),
+                        at_ ? (const int32_t *)at_->data_ptr() : nullptr, (int32_t)T, half_ptr(q), q ? q->stride(0) : 0,
+                        (int32_t)heads, q ? half_out(out) : nullptr, q ? out.stride(0) : 0, stream);
+    Py_END_ALLOW_THREADS
     if (st != PARO_OK) return PyLong_FromLong(st);
     if (!q) Py_RETURN_NONE;
     return wrap(a[7], std::move(out));
@@ -321,9 +340,13 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     at::Tensor o = rows_or_new(a[8], B, q->size(1), *q), lse;
     if (!o.defined()) return nullptr;
     if (want) lse = fresh(*q, {B, heads}, at::kFloat);
-    const paro_status st = paro_paged_attention(c, half_ptr(q), q->stride(0), (int32_t)heads, (const int32_t *)table->data_ptr(), ld,
-                                                (int32_t)table->size(1), (const int32_t *)lengths->data_ptr(), (int32_t)B, scale, window, half_out(o),
-                                                o.stride(0), want ? (float *)lse.data_ptr() : nullptr, ws->data_ptr(), bytes, current_stream());
+    void *stream = current_stream();
+    paro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = paro_paged_attention(c, half_ptr(q), q->stride(0), (int32_t)heads, (const int32_t *)table->data_ptr(), ld,
+                              (int32_t)table->size(1), (const int32_t *)lengths->data_ptr(), (int32_t)B, scale, window, half_out(o),
+                              o.stride(0), want ? (float *)lse.data_ptr() : nullptr, ws->data_ptr(), bytes, stream);
+    Py_END_ALLOW_THREADS
     if (st != PARO_OK) return PyLong_FromLong(st);
     PyObject *first = wrap(a[8], std::move(o));
     return want ? together({first, THPVariable_Wrap(std::move(lse))}) : first;

@@ -800,7 +800,7 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     if (!Q || !O || !block_table || !lengths) return PARO_ERR_NULL;
     const paro_kv_cache &c = *cache;
     if (batch <= 0 || q_heads <= 0 || q_heads % c.kv_heads || table_width <= 0 || window < 0) return PARO_ERR_SHAPE;
-    if (ld_table != 0 && ld_table < table_width) return PARO_ERR_SHAPE;
+    if ((ld_table != 0 && ld_table < table_width) || O == Q) return PARO_ERR_SHAPE;
     if (!std::isfinite(scale * kLog2e)) return PARO_ERR_SHAPE;
     if (const paro_status st = check_rows(Q, ldq, (int64_t)q_heads * c.head_dim); st != PARO_OK) return st;
     if (const paro_status st = check_rows(O, ldo, (int64_t)q_heads * c.head_dim); st != PARO_OK) return st;

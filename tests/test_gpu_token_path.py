@@ -426,17 +426,19 @@ def test_attention_special_scores(P, fmt):
         assert bool(torch.isfinite(o).all())                           # the NaN is past the end
 
 
-def test_numbers_beyond_32_bits_are_refused(P):
+def test_refusals_of_the_calls(P):
     import torch
     from paper_2511_10645_amd import binding as B_
-    say("numbers beyond 32 bits, in both bindings")
+    say("numbers beyond 32 bits, outputs without their inputs, other shapes, in both bindings")
     cache, table, q, _ = _attn(P, [20], 2, 1, 64, 16, "fp16", 1)
     x, w = torch.zeros((2, 128), dtype=torch.float16, device="cuda"), torch.ones(128, dtype=torch.float16, device="cuda")
     native = B_._native()
     try:
         for B_._host in (native, B_._CtypesCalls):
             for call in (lambda: P.paro_paged_attention(cache, cuda(q), cuda(table), cuda(np.array([20], np.int32)), ws_of(P, cache, 2, 1), window=2 ** 32 + 1),
-                         lambda: P.paro_rms_norm_quantize_e4m3(x, w, 1e-5, group=2 ** 32 + 128)):
+                         lambda: P.paro_rms_norm_quantize_e4m3(x, w, 1e-5, group=2 ** 32 + 128), lambda: P.paro_rms_norm(x, w, 1e-5, H=x),
+                         lambda: P.paro_rms_norm_quantize_e4m3(x, w, 1e-5, H=x), lambda: P.paro_rms_norm(x, w, 1e-5, residual=x[:1]),
+                         lambda: P.paro_kv_append(cache, x[:, :64], x[:, :64], torch.zeros(2, dtype=torch.int64, device="cuda"), Qr=x)):
                 with pytest.raises(AssertionError):
                     call()
             with pytest.raises(P.ParoError):

@@ -64,10 +64,11 @@ def test_rope_and_append_refusals():
 def test_attention_refusals_and_workspace():
     L = paro.lib()
     need = L.paro_workspace_bytes_attention(r(_cache()), 8, 3)
-    f = lambda c=_cache(), Q=FAKE, ldq=1024, hq=8, table=FAKE, ldt=4, width=4, lengths=FAKE, batch=3, scale=0.1, window=0, O=FAKE, ldo=1024, lse=None, ws=FAKE, n=need: \
+    f = lambda c=_cache(), Q=FAKE, ldq=1024, hq=8, table=FAKE, ldt=4, width=4, lengths=FAKE, batch=3, scale=0.1, window=0, O=FAKE * 4, ldo=1024, lse=None, ws=FAKE, n=need: \
         L.paro_paged_attention(r(c) if c else None, Q, ldq, hq, table, ldt, width, lengths, batch, scale, window, O, ldo, lse, ws, n, None)
     assert f(c=None) == E_NULL and f(Q=None) == E_NULL and f(O=None) == E_NULL and f(table=None) == E_NULL and f(lengths=None) == E_NULL
     assert f(batch=0) == E_SHAPE and f(hq=7) == E_SHAPE and f(hq=0) == E_SHAPE and f(width=0) == E_SHAPE and f(window=-1) == E_SHAPE and f(ldt=3) == E_SHAPE
+    assert f(O=FAKE) == E_SHAPE                                         # the queries themselves
     assert f(scale=3e38) == E_SHAPE                                     # finite, but not in units of log2
     assert f(scale=math.nan) == E_SHAPE and f(scale=math.inf) == E_SHAPE and f(ldq=512) == E_SHAPE and f(ldo=512) == E_SHAPE
     assert f(Q=FAKE + 2) == E_ALIGN and f(ldo=1028) == E_ALIGN and f(lse=FAKE + 2) == E_ALIGN and f(ws=FAKE + 128) == E_ALIGN and f(lengths=FAKE + 1) == E_ALIGN
