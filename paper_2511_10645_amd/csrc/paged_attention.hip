@@ -46,6 +46,14 @@ typedef uint32_t U2 __attribute__((ext_vector_type(2)));
 // waves of a block: two for every SIMD, one where a wave's registers are more than half of them
 template <int D> constexpr int attn_waves() { return D == 256 ? 4 : 8; }
 
+// Blocks for a head of one sequence of `units` units: one where its waves can take a unit each, then at most as many as are joined
+// in one round, and twice that for long ones.
+__host__ __device__ constexpr uint32_t one_parts(uint32_t units, uint32_t waves)
+{
+    const uint32_t parts = (units + kLeastUnits - 1) / kLeastUnits, most = units <= 64 ? 8 : 16;
+    return units <= waves ? 1 : parts < most ? parts : most;
+}
+
 struct AttnArgs {
     const uint8_t *k, *v, *ks, *vs;
     const _Float16 *q;
@@ -522,20 +530,29 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         pl.length = n;
     }
     upto = sums_upto(upto);
-    const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
+    uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
     // Units of a block and of a wave: all waves of the grid alike; where that would leave a block fewer than kLeastUnits, fewer blocks.
     uint32_t share = quotient(total + gridDim.x - 1, gridDim.x, a.per_block), mine = 1;
     if (share < kLeastUnits) share = kLeastUnits;
+    // One sequence of some thousand tokens at most: every head begins with a block of its own (segments are numbered `pitch` apart), so that
+    // its parts are as few and as even as can be, and a head of up to WAVES units stays in one block (200 tokens: 9.1 -> 6.2 us).
     const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);
-    if (a.batch == 1 && share < one && one <= WAVES)
-        share = one;                             // one short sequence: a head in one block, nothing goes through memory (200 tokens: 9.1 -> 6.7 us)
-    else if (share >= WAVES) {
-        mine = (share + WAVES - 1) / WAVES;
-        share = mine * WAVES;
+    uint32_t pitch = 0, head_end = total;
+    if (a.batch == 1) {
+        const uint32_t parts = one_parts(one, WAVES);
+        if (share <= WAVES && hc * parts <= gridDim.x) {
+            const float per_parts = __builtin_amdgcn_rcpf((float)parts);
+            share = quotient(one + parts - 1, parts, per_parts);
+            pitch = parts * share;
+            total = pitch * hc;
+            head_end = quotient(blockIdx.x, parts, per_parts) * pitch + one;
+        }
     }
+    if (share >= WAVES || pitch) mine = (share + WAVES - 1) / WAVES;
+    if (share >= WAVES && !pitch) share = mine * WAVES;
     const uint32_t begin = blockIdx.x * share;
     if (begin >= total) return;
-    const uint32_t end = begin + share < total ? begin + share : total;
+    const uint32_t end = begin + share < head_end ? begin + share : head_end;
     const uint32_t wbegin = begin + wave * mine, wend = wbegin + mine < end ? wbegin + mine : end;
     const float per_share = __builtin_amdgcn_rcpf((float)share);
 
@@ -546,7 +563,9 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     if (busy) {
         pl.base = 0;
         pl.first = 0;
-        if (per == 1) {
+        if (pitch) {
+            pl.sequence(a, 0, lane);
+        } else if (per == 1) {
             pl.find(a, wbegin, upto, hc, lane);
         } else {                                 // the lane whose sequences hold unit wbegin, and these one to a lane
             const int before = __popcll(__ballot(upto * hc <= wbegin));
@@ -574,13 +593,14 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         pages = hi > 0 ? row[t >> a.page_log] : 0;
     };
     const auto locate = [&](uint32_t at) {
-        while (pl.base + (uint32_t)pl.sp.units * hc <= at) pl.next(a, lane, hc);
+        if (!pitch)
+            while (pl.base + (uint32_t)pl.sp.units * hc <= at) pl.next(a, lane, hc);
         lo = pl.sp.lo; hi = pl.sp.hi;
         row = a.table + (int64_t)pl.b * a.ld_table;
-        const uint32_t units = (uint32_t)pl.sp.units;
+        const uint32_t units = (uint32_t)pl.sp.units, apart = pitch ? pitch : units;
         g.b = pl.b;
-        g.seg = (int)quotient(at - pl.base, units, __builtin_amdgcn_rcpf((float)units));
-        g.seg0 = pl.base + (uint32_t)g.seg * units;
+        g.seg = (int)quotient(at - pl.base, apart, __builtin_amdgcn_rcpf((float)apart));
+        g.seg0 = pl.base + (uint32_t)g.seg * apart;
         g.seg1 = g.seg0 + units;
         u0 = pl.sp.unit0 + (int)(at - g.seg0);
         u1 = pl.sp.unit0 + (int)((g.seg1 < wend ? g.seg1 : wend) - g.seg0);
@@ -756,8 +776,10 @@ template <int D, int FMT>
 static hipError_t launch_attention(AttnArgs &a, int64_t units, hipStream_t s)
 {
     constexpr int WAVES = attn_waves<D>();
-    // no more blocks than the longest sequences could have units for
-    const int64_t most = (units + kLeastUnits - 1) / kLeastUnits;
+    // no more blocks than the longest sequences could have units for, and a single one's heads blocks of their own
+    int64_t most = (units + kLeastUnits - 1) / kLeastUnits;
+    const int64_t heads = (int64_t)a.kv_heads * a.chunks;
+    if (const int64_t apart = heads * one_parts((uint32_t)(units / heads), WAVES); a.batch == 1 && most < apart) most = apart;
     const unsigned blocks = (unsigned)(most < kAttnBlocks ? most : kAttnBlocks);
     a.per_block = 1.0f / (float)blocks;
     const int rows = a.group < kQueries ? a.group : kQueries;

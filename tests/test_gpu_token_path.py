@@ -335,6 +335,18 @@ def test_attention_split_and_joined(P, n, hq, hkv, D, page, fmt):
     assert (o == again).all() and (lse == lse2).all()                  # not a matter of timing
 
 
+@pytest.mark.parametrize("hq,hkv,D,fmt", [(4, 1, 64, "fp16"), (6, 2, 128, "e4m3"), (16, 16, 64, "fp16"), (33, 33, 64, "fp16"), (20, 1, 128, "fp16"), (4, 2, 256, "fp16"),
+                                         (300, 300, 64, "e4m3")])
+def test_attention_one_sequence(P, hq, hkv, D, fmt):
+    """One sequence of lengths around the numbers of units at which a head takes another number of blocks, in a table that is wider."""
+    say(f"attention of one sequence, {hq}/{hkv} x {D} {fmt}")
+    lengths = [1, 32, 33, 128, 129, 160, 256, 257, 289, 383, 511, 1025] if hkv > 30 else [1, 33, 129, 160, 256, 257, 289, 383, 511, 700, 1200, 2047, 2049, 4100, 6001]
+    cache, table, q, rows = _attn(P, [lengths[-1]], hq, hkv, D, 16, fmt, hq)
+    for n in lengths:
+        _check(P, cache, table, q, rows if n == lengths[-1] else [(rows[0][0][:n], rows[0][1][:n])], [n], hq, D ** -0.5)
+    _check(P, cache, table, q, [(rows[0][0][:1000], rows[0][1][:1000])], [1000], hq, D ** -0.5, window=300)
+
+
 @pytest.mark.parametrize("B", [64, 65, 150, 700, 4500])
 def test_attention_many_ragged(P, B):
     say(f"attention of {B} sequences")
