@@ -256,7 +256,7 @@ def _native():
             paro_host.types(_CRotation, _CW4Weight)
             paro_host.token_types(_CRope, _CKVCache)
             _host = paro_host
-        except ImportError as e:
+        except (ImportError, AttributeError) as e:      # not built, or built against another torch or for other calls
             if os.path.exists(_HOST_PATH):
                 warnings.warn(f"paro_host.so does not load, calls go through ctypes: {e}")
             _host = _CtypesCalls

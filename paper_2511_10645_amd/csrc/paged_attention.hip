@@ -523,11 +523,15 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     Place pl;
     const int per = (a.batch + 63) >> 6;
     uint32_t upto = 0;
+    if (per == 1) {
+        pl.lanes(a, 0, lane);
+        upto = lane < a.batch ? (uint32_t)span_of(a, pl.length).units : 0u;
+    } else {
 #pragma unroll 4
-    for (int j = 0; j < per; ++j) {
-        const int i = lane * per + j, n = a.lengths[i < a.batch ? i : a.batch - 1];
-        upto += i < a.batch ? (uint32_t)span_of(a, n).units : 0u;
-        pl.length = n;
+        for (int j = 0; j < per; ++j) {
+            const int i = lane * per + j, n = a.lengths[i < a.batch ? i : a.batch - 1];
+            upto += i < a.batch ? (uint32_t)span_of(a, n).units : 0u;
+        }
     }
     upto = sums_upto(upto);
     uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * hc;
@@ -562,7 +566,6 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     const bool busy = wbegin < wend;
     if (busy) {
         pl.base = 0;
-        pl.first = 0;
         if (pitch) {
             pl.sequence(a, 0, lane);
         } else if (per == 1) {
