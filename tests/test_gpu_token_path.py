@@ -165,7 +165,9 @@ def _append_case(P, T, hq, hkv, D, page, fmt, seed, rot=None, layout="halves", s
 @pytest.mark.parametrize("T,hq,hkv,D,page,fmt,rot,layout", [
     (1, 8, 2, 128, 16, "fp16", 128, "halves"), (1, 8, 2, 128, 16, "e4m3", 128, "halves"), (37, 4, 4, 64, 32, "fp16", 16, "interleaved"),
     (37, 4, 4, 64, 32, "e4m3", 48, "halves"), (300, 5, 1, 128, 64, "fp16", 64, "halves"), (300, 5, 1, 128, 64, "e4m3", 128, "interleaved"),
-    (19, 16, 2, 256, 16, "fp16", 256, "halves"), (261, 3, 3, 256, 1024, "e4m3", 64, "interleaved"), (70, 8, 8, 128, 16, "e4m3", 32, "halves")])
+    (19, 16, 2, 256, 16, "fp16", 256, "halves"), (261, 3, 3, 256, 1024, "e4m3", 64, "interleaved"), (70, 8, 8, 128, 16, "e4m3", 32, "halves"),
+    (1030, 4, 2, 128, 16, "fp16", 128, "halves"), (1031, 3, 1, 64, 32, "e4m3", 64, "interleaved"), (1025, 10, 2, 128, 16, "e4m3", 96, "halves"),
+    (1024, 2, 2, 256, 64, "fp16", 128, "interleaved")])
 def test_append(P, T, hq, hkv, D, page, fmt, rot, layout):
     say(f"append {T} tokens, {hq}/{hkv} x {D}, page {page} {fmt}, {rot} {layout}")
     cache, rope, f, slots, qkv, pos = _append_case(P, T, hq, hkv, D, page, fmt, T + D, rot, layout)
@@ -221,6 +223,7 @@ def test_append_leaves_out_and_in_place(P, fmt):
         assert np.abs(k_got - k3).max() < 0.07 * np.abs(k3).max() and np.abs(v_got - v3).max() < 0.07 * np.abs(v3).max()
     touched = (cache.v != before).any(-1).any(1).flatten().cpu().numpy()
     assert set(np.nonzero(touched)[0]) <= set(slots[kept].tolist())
+    assert (P.paro_kv_append(cache, k, v, cuda(slots), Q=q) == q).all()        # no rotation: queries as they are
     want = P.paro_kv_append(cache, k, v, cuda(slots), rope, cuda(pos), q)
     assert P.paro_kv_append(cache, k, v, cuda(slots), rope, cuda(pos), q, q) is not None
     assert (x[:, :hq * D] == want).all()
