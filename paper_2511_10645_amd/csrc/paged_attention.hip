@@ -304,11 +304,12 @@ __device__ inline void take_in(Running<D> &st, const float (&x)[8], const Values
         for (int r = 0; r < R; ++r) st.acc[r] *= f;
         st.m = top;
     }
-    const float off = (st.m == -INFINITY ? 0.0f : st.m) - kPShift;
+    // The shift goes onto the difference: off a maximum of 2^24 and more, 15 is rounded to 16, and 2^16 is not an fp16 number.
+    const float ref = st.m == -INFINITY ? 0.0f : st.m;
     half8v p, rest;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float e = __builtin_amdgcn_exp2f(x[j] - off);
+        const float e = __builtin_amdgcn_exp2f((x[j] - ref) + kPShift);
         st.l += e;
         p[j] = (_Float16)e;
         rest[j] = (_Float16)(e - (float)p[j]);

@@ -1,0 +1,36 @@
+"""The operators between the linears where their arithmetic, their split or their arguments come to an end; bounds: token_path_ref.py."""
+import numpy as np
+import pytest
+
+import test_gpu_token_path as base
+import token_path_ref as ref
+
+pytestmark = pytest.mark.gpu
+cuda, say, within, ws_of = base.cuda, base.say, base.within, base.ws_of
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2511_10645_amd as paro
+    return paro
+
+
+@pytest.mark.parametrize("n", [96, 5000])
+@pytest.mark.parametrize("scale", [1e6, 1.2e7, 2e7, 5e7, 1e8, 1.5e8, 3e8, 1e9, 1e30, -2e7, -1e8])
+def test_attention_huge_finite_scores(P, n, scale):
+    """Scores are +scale and -scale by turns: equal weights for one half, none for the other.  Bound: the n/2 equal terms are exact and
+    summed in fp32, (n/2) 2^-24 of their mean size at most; lse passes five fp32 roundings."""
+    say(f"attention of {n} tokens, scores +-{scale:g}")
+    D = 64
+    rs = np.random.default_rng(n)
+    cache = P.KVCache(-(-n // 16), 1, D, 16)
+    k, v, q = np.zeros((n, D), np.float16), rs.standard_normal((n, D)).astype(np.float16), np.zeros((1, D), np.float16)
+    k[::2, 0], k[1::2, 0], q[0, 0] = 1, -1, 1
+    P.paro_kv_append(cache, cuda(k), cuda(v), cuda(np.arange(n, dtype=np.int64)))
+    table = cuda(np.arange(-(-n // 16), dtype=np.int32)[None])
+    o, lse = P.paro_paged_attention(cache, cuda(q), table, cuda(np.array([n], np.int32)), ws_of(P, cache, 1, 1), scale, with_lse=True)
+    half = v[0 if scale > 0 else 1::2].astype(np.float64)
+    want = half.mean(0)
+    within(o.cpu().numpy()[0], want, ref.F16 * np.abs(want) + ref.TINY + n / 2 * 2.0 ** -24 * np.abs(half).mean(0), "o")
+    l_want = abs(scale) + np.log(n / 2)
+    within(lse.cpu().numpy()[0], np.array([l_want]), np.array([2.0 ** -21 * l_want + 2.0 ** -20]), "lse")
