@@ -111,7 +111,8 @@ __global__ __launch_bounds__(LANES < kNormThreads ? kNormThreads : LANES) void n
             // a maximum below the floor of 1e-30 / 448 takes that scale
             const float scale = fmaxf(m * inv, 1e-30f) / kE4m3Max;
             const float least = inv * (kE4m3Max / 1e-30f);
-            const float up = m * inv > 1e-30f ? kE4m3Max / m : least > 3e38f ? 3e38f : least;      // NaN stays NaN
+            // no norm at all (a row of zeros without eps, or NaN in it): every code is NaN
+            const float up = m * inv > 1e-30f ? kE4m3Max / m : is_finite(inv) ? fminf(least, 3e38f) : NAN;
             float q[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

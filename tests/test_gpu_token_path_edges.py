@@ -34,3 +34,25 @@ def test_attention_huge_finite_scores(P, n, scale):
     within(o.cpu().numpy()[0], want, ref.F16 * np.abs(want) + ref.TINY + n / 2 * 2.0 ** -24 * np.abs(half).mean(0), "o")
     l_want = abs(scale) + np.log(n / 2)
     within(lse.cpu().numpy()[0], np.array([l_want]), np.array([2.0 ** -21 * l_want + 2.0 ** -20]), "lse")
+
+
+@pytest.mark.parametrize("C", [128, 1024, 4096, 32768])
+def test_norm_of_zeros_without_eps(P, C):
+    """0 / 0 in both forms; with eps the row is zeros, and other rows are what they are."""
+    import torch
+    say(f"norm of a row of zeros, {C} channels")
+    x, w = torch.ones((3, C), dtype=torch.float16, device="cuda"), torch.full((C,), 0.5, dtype=torch.float16, device="cuda")
+    x[1] = 0
+    r = -x
+    r[0] = r[2] = 0
+    for residual in (None, r):
+        got = P.paro_rms_norm(x, w, 0.0, residual=residual)
+        y = got if residual is None else got[0]
+        assert bool(y[1].isnan().all()) and bool((y[[0, 2]] == 0.5).all())
+        for group in (0, 128):
+            codes, scales = P.paro_rms_norm_quantize_e4m3(x, w, 0.0, group, residual=residual)[:2]
+            codes = codes.cpu().numpy()
+            assert (codes[1] & 127 == 127).all() and (codes[[0, 2]] == 126).all()           # NaN; 448
+            within(scales[[0, 2]].cpu().numpy(), np.full((2, scales.shape[1]), 0.5 / 448), np.full((1, 1), 2.0 ** -18 * 0.5 / 448), "scales")
+            codes = P.paro_rms_norm_quantize_e4m3(x, w, 1e-5, group, residual=residual)[0]
+            assert not bool(codes[1].any())
