@@ -776,6 +776,15 @@ static int attn_chunks(const paro_kv_cache &c, int q_heads) { return (q_heads / 
 static size_t attn_part_bytes(const paro_kv_cache &c) { return sizeof(float) * kQueries * (c.head_dim + 4); }
 static size_t attn_scratch_bytes(const paro_kv_cache &c) { return ((size_t)2 * kAttnBlocks * attn_part_bytes(c) + 255) / 256 * 256; }
 
+// Most units of a head whose sequence has up to `tokens` tokens, of which `window` (0: all) are attended to.
+static constexpr int64_t units_seen(int64_t tokens, int32_t window)
+{
+    const int64_t within = (int64_t)window + 2 * kUnit;
+    return ((window > 0 && within < tokens ? within : tokens) + kUnit - 1) / kUnit;
+}
+static_assert(units_seen(4096, INT32_MAX) == 128 && units_seen(4096, 0) == 128 && units_seen(4096, 1) == 3 && units_seen(1, 1) == 1,
+              "any window that an int32 holds");
+
 template <int D, int FMT>
 static hipError_t launch_attention(AttnArgs &a, int64_t units, hipStream_t s)
 {
@@ -849,9 +858,7 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     a.page_log = log2_of(c.page); a.n_pages = c.n_pages; a.kv_heads = c.kv_heads; a.group = q_heads / c.kv_heads;
     a.chunks = attn_chunks(c, q_heads); a.width = table_width; a.batch = batch; a.window = window;
     a.scale = scale * kLog2e;
-    int64_t seen = tokens;
-    if (window > 0 && window + 2 * kUnit < seen) seen = window + 2 * kUnit;
-    const int64_t most = units * ((seen + kUnit - 1) / kUnit);
+    const int64_t most = units * units_seen(tokens, window);
     hipStream_t s = (hipStream_t)stream;
     hipError_t e;
     switch (c.head_dim * 2 + c.format) {

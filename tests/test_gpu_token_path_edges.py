@@ -56,3 +56,13 @@ def test_norm_of_zeros_without_eps(P, C):
             within(scales[[0, 2]].cpu().numpy(), np.full((2, scales.shape[1]), 0.5 / 448), np.full((1, 1), 2.0 ** -18 * 0.5 / 448), "scales")
             codes = P.paro_rms_norm_quantize_e4m3(x, w, 1e-5, group, residual=residual)[0]
             assert not bool(codes[1].any())
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 64, 4097])
+def test_attention_window_beyond_every_token(P, window):
+    say(f"attention within {window}")
+    lengths = [0, 1, 700, 4096] + [33] * 20
+    cache, table, q, rows = base._attn(P, lengths, 8, 4, 64, 16, "fp16", 8)
+    o, lse = base._check(P, cache, table, q, rows, lengths, 8, 0.125, window)
+    whole, lse_whole = base._check(P, cache, table, q, rows, lengths, 8, 0.125)
+    assert (o == whole).all() and (lse == lse_whole).all()
