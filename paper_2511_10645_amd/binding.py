@@ -47,15 +47,17 @@ class _CMxfp4Weight(ctypes.Structure):
     ]
 
 
+# These two end in the GPU that their memory is on (-1: host memory), which the calls compare with their tensors'; the library does not read it.
 class _CRope(ctypes.Structure):
     _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float),
-                ("inv_freq", ctypes.c_void_p)]
+                ("inv_freq", ctypes.c_void_p), ("device", ctypes.c_int32)]
 
 
 class _CKVCache(ctypes.Structure):
     _fields_ = [
         ("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32),
         ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("device", ctypes.c_int32),
     ]
 
 
@@ -174,9 +176,10 @@ class _CtypesCalls:
     def rms_norm(X, w, eps, R, Y, H):
         ldx = _gpu_rows(X)
         T, C = X.shape
-        _gpu_vector(w, torch.float16, C)
+        _gpu_vector(w, torch.float16, C, X)
         assert R is not None or H is None, "H takes the sum with a residual"
-        ldr = 0 if R is None else _gpu_rows(R, T, C)
+        ldr = 0 if R is None else _gpu_rows(R, T, C, X)
+        _current(X)
         Y, ldy = _rows_or_new(Y, T, C, X)
         H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
         st = lib().paro_rms_norm(X.data_ptr(), ldx, _ptr(R), ldr, w.data_ptr(), eps, T, C, _ptr(H), ldh, Y.data_ptr(), ldy, _stream())
@@ -186,9 +189,10 @@ class _CtypesCalls:
     def rms_norm_quantize_e4m3(X, w, eps, group, R, H):
         ldx = _gpu_rows(X)
         T, C = X.shape
-        _gpu_vector(w, torch.float16, C)
+        _gpu_vector(w, torch.float16, C, X)
         assert R is not None or H is None, "H takes the sum with a residual"
-        ldr = 0 if R is None else _gpu_rows(R, T, C)
+        ldr = 0 if R is None else _gpu_rows(R, T, C, X)
+        _current(X)
         H, ldh = (None, 0) if R is None else _rows_or_new(H, T, C, X)
         _number(group)
         codes = torch.empty((T, C), dtype=torch.uint8, device=X.device)
@@ -201,7 +205,9 @@ class _CtypesCalls:
     def rope(rope, X, positions, Y):
         ldx = _gpu_rows(X)
         T, C = X.shape
-        _gpu_vector(positions, torch.int32, T)
+        _gpu_vector(positions, torch.int32, T, X)
+        _same_gpu(rope.device, X)
+        _current(X)
         assert C % rope.head_dim == 0, "rows are not whole heads"
         Y, ldy = _rows_or_new(Y, T, C, X)
         st = lib().paro_rope(ctypes.byref(rope), X.data_ptr(), ldx, positions.data_ptr(), C // rope.head_dim, T, Y.data_ptr(), ldy, _stream())
@@ -212,14 +218,18 @@ class _CtypesCalls:
         width = cache.kv_heads * cache.head_dim
         ldk = _gpu_rows(K, -1, width)
         T = K.shape[0]
-        ldv = _gpu_rows(V, T, width)
-        _gpu_vector(slots, torch.int64, T)
+        ldv = _gpu_rows(V, T, width, K)
+        _gpu_vector(slots, torch.int64, T, K)
         if positions is not None:
-            _gpu_vector(positions, torch.int32, T)
+            _gpu_vector(positions, torch.int32, T, K)
+        _same_gpu(cache.device, K)
+        if rope is not None:
+            _same_gpu(rope.device, K)
+        ldq = 0 if Q is None else _gpu_rows(Q, T, like=K)
+        _current(K)
         assert Q is not None or Qr is None, "Qr takes rotated queries, and there are none"
-        ldq = ldqr = heads = 0
+        ldqr = heads = 0
         if Q is not None:
-            ldq = _gpu_rows(Q, T)
             assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
             heads = Q.shape[1] // cache.head_dim
             Qr, ldqr = _rows_or_new(Qr, T, Q.shape[1], Q)
@@ -232,9 +242,13 @@ class _CtypesCalls:
         ldq = _gpu_rows(Q)
         B = Q.shape[0]
         assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
-        assert table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.shape[0] == B and table.is_cuda
-        _gpu_vector(lengths, torch.int32, B)
-        assert buf.is_cuda and table.shape[1] < 2 ** 31
+        assert table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.shape[0] == B
+        _gpu_vector(lengths, torch.int32, B, Q)
+        assert table.is_cuda and buf.is_cuda, "expected a tensor on the GPU"
+        for device in (table.device.index, buf.device.index, cache.device):
+            _same_gpu(device, Q)
+        _current(Q)
+        assert table.shape[1] < 2 ** 31
         _number(window)
         heads = Q.shape[1] // cache.head_dim
         O, ldo = _rows_or_new(O, B, Q.shape[1], Q)
@@ -487,18 +501,35 @@ def _rows(x: torch.Tensor):
     return x.shape[0], x.stride(0)
 
 
-def _gpu_rows(x: torch.Tensor, T: int = -1, width: int | None = None) -> int:
-    """The row stride of fp16 rows on the GPU, checked as the native calls check them."""
+def _same_gpu(device: int, first: torch.Tensor) -> None:
+    assert device == first.device.index, "expected tensors, cache and frequencies on one GPU"
+
+
+def _current(first: torch.Tensor) -> None:
+    assert first.device.index == torch.cuda.current_device(), "the tensors' GPU is not the current one"
+
+
+def _gpu_rows(x: torch.Tensor, T: int = -1, width: int | None = None, like: torch.Tensor | None = None) -> int:
+    """The row stride of fp16 rows on the GPU (that of `like`), checked as the native calls check them."""
     rows, ld = _rows(x)
     assert x.is_cuda, "expected a tensor on the GPU"
+    if like is not None:
+        _same_gpu(x.device.index, like)
     assert rows < 2 ** 31, "more rows than 32 bits count"
     assert (T < 0 or rows == T) and (width is None or x.shape[1] == width), "tensors of different shapes"
     return ld
 
 
-def _gpu_vector(x: torch.Tensor, dtype, n: int) -> None:
+def _gpu_vector(x: torch.Tensor, dtype, n: int, like: torch.Tensor) -> None:
     assert x.dtype == dtype and x.dim() == 1 and x.is_contiguous() and x.shape[0] == n, "expected a contiguous vector of another type or length"
     assert x.is_cuda, "expected a tensor on the GPU"
+    _same_gpu(x.device.index, like)
+
+
+def _device_of(*tensors) -> int:
+    """The GPU that all of these are on, -1 for host memory."""
+    assert all(x.device == tensors[0].device for x in tensors), "tensors on different devices"
+    return tensors[0].device.index if tensors[0].is_cuda else -1
 
 
 def _number(n: int) -> None:
@@ -508,7 +539,7 @@ def _number(n: int) -> None:
 def _rows_or_new(x, T: int, width: int, like: torch.Tensor):
     if x is None:
         return torch.empty((T, width), dtype=torch.float16, device=like.device), width
-    return x, _gpu_rows(x, T, width)
+    return x, _gpu_rows(x, T, width, like)
 
 
 def paro_rotate_scale(rot: Rotation, X: torch.Tensor, Xr: torch.Tensor | None = None) -> torch.Tensor:
@@ -716,14 +747,17 @@ def paro_rope_frequencies_host(rot_dim: int, base: float = 10000.0, scaling: str
 
 
 class Rope:
-    """Rotary positions of heads (struct paro_rope_t): inv_freq fp32 [rot_dim/2] (tensor or array), the first rot_dim channels rotated."""
+    """Rotary positions of heads (struct paro_rope_t): inv_freq fp32 [rot_dim/2] (a tensor, moved unless it is on a device of this type, or an
+    array), the first rot_dim channels rotated."""
 
     def __init__(self, inv_freq, head_dim: int, layout: str = "halves", magnitude: float = 1.0, device="cuda"):
         if not isinstance(inv_freq, torch.Tensor):
-            inv_freq = torch.as_tensor(np.ascontiguousarray(inv_freq, dtype=np.float32)).to(device)
+            inv_freq = torch.as_tensor(np.ascontiguousarray(inv_freq, dtype=np.float32))
+        if inv_freq.device.type != torch.device(device).type:
+            inv_freq = inv_freq.to(device)
         assert inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()
         self.inv_freq, self.head_dim, self.rot_dim = inv_freq, head_dim, 2 * inv_freq.shape[0]
-        self.c = _CRope(head_dim, self.rot_dim, ROPE_LAYOUTS[layout], magnitude, _ptr(inv_freq))
+        self.c = _CRope(head_dim, self.rot_dim, ROPE_LAYOUTS[layout], magnitude, _ptr(inv_freq), _device_of(inv_freq))
 
     def ref(self):
         return ctypes.byref(self.c)
@@ -753,6 +787,7 @@ class KVCache:
         return self
 
     def _take(self, k, v, k_scale, v_scale):
+        assert (k_scale is None) == (v_scale is None), "scales of both keys and values, or of neither"
         e4m3 = k_scale is not None
         self.n_pages, self.kv_heads, self.page, self.head_dim = v.shape
         u = 16 if e4m3 else 8
@@ -762,7 +797,8 @@ class KVCache:
             assert s.dtype == torch.uint8 and s.is_contiguous() and s.shape == (self.n_pages, self.kv_heads, self.page)
         self.format = "e4m3" if e4m3 else "fp16"
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.c = _CKVCache(self.n_pages, self.page, self.kv_heads, self.head_dim, int(e4m3), _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+        self.c = _CKVCache(self.n_pages, self.page, self.kv_heads, self.head_dim, int(e4m3), _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale),
+                         _device_of(k, v, *((k_scale, v_scale) if e4m3 else ())))
 
     def ref(self):
         return ctypes.byref(self.c)

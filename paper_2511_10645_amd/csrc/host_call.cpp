@@ -137,19 +137,30 @@ bool refuse(const char *why)
     return false;
 }
 
-// fp16 rows of `width` channels on the GPU; `t` tokens (-1: any)
-bool gpu_rows(const at::Tensor &x, int64_t t, int64_t width)
+// A call's tensors, its cache and its frequencies are on the GPU of its first tensor, and that GPU is the current one: the
+// kernels go to the current stream and follow the pointers of all.
+struct RopeOn { paro_rope_t c; int32_t device; };               // _CRope, _CKVCache: -1 in host memory
+struct CacheOn { paro_kv_cache c; int32_t device; };
+bool same_gpu(int device, const at::Tensor &first) { return device == first.device().index() || refuse("expected tensors, cache and frequencies on one GPU"); }
+bool on_gpu(const at::Tensor &x, const at::Tensor &first)
 {
-    if (!rows(x)) return false;
     if (!x.is_cuda()) return refuse("expected a tensor on the GPU");
+    return same_gpu(x.device().index(), first);
+}
+bool current(const at::Tensor &first) { return first.device().index() == c10::hip::current_device() || refuse("the tensors' GPU is not the current one"); }
+
+// fp16 rows of `width` channels on the GPU of `first`; `t` tokens (-1: any)
+bool gpu_rows(const at::Tensor &x, int64_t t, int64_t width, const at::Tensor &first)
+{
+    if (!rows(x) || !on_gpu(x, first)) return false;
     if (x.size(0) > INT32_MAX) return refuse("more rows than 32 bits count");
     if ((t >= 0 && x.size(0) != t) || x.size(1) != width) return refuse("tensors of different shapes");
     return true;
 }
-bool gpu_vector(const at::Tensor &x, at::ScalarType type, int64_t n)
+bool gpu_vector(const at::Tensor &x, at::ScalarType type, int64_t n, const at::Tensor &first)
 {
     if (x.scalar_type() != type || x.dim() != 1 || !x.is_contiguous() || x.size(0) != n) return refuse("expected a contiguous vector of another type or length");
-    return x.is_cuda() || refuse("expected a tensor on the GPU");
+    return on_gpu(x, first);
 }
 // A number of 32 bits; false with an exception set if it is none.
 bool number(PyObject *o, int32_t &to)
@@ -165,11 +176,11 @@ bool maybe(PyObject *o, const at::Tensor *&t)
     t = nullptr;
     return o == Py_None || (t = tensor(o));
 }
-// A new dense tensor where `like` is, from the allocator that `like` came from: 0.3 us of host time, 0.85 by way of the dispatcher.
+// A new dense tensor where `like` is (the current GPU), from the allocator that `like` came from: 0.3 us of host time, 0.85 by way of the dispatcher.
 at::Tensor fresh(const at::Tensor &like, at::IntArrayRef sizes, at::ScalarType type)
 {
     c10::Allocator *allocator = like.storage().allocator();
-    if (!allocator || like.device().index() != c10::hip::current_device()) return at::empty(sizes, like.options().dtype(type).requires_grad(false));
+    if (!allocator) return at::empty(sizes, like.options().dtype(type).requires_grad(false));
     return at::Tensor(at::detail::empty_generic(sizes, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));
 }
 // `o` if given, else new rows; undefined with an exception set on failure
@@ -177,7 +188,7 @@ at::Tensor rows_or_new(PyObject *o, int64_t t, int64_t width, const at::Tensor &
 {
     if (o == Py_None) return fresh(like, {t, width}, at::kHalf);
     const at::Tensor *x = tensor(o);
-    return x && gpu_rows(*x, t, width) ? *x : at::Tensor();
+    return x && gpu_rows(*x, t, width, like) ? *x : at::Tensor();
 }
 const paro_half_t *half_ptr(const at::Tensor *t) { return t ? (const paro_half_t *)t->data_ptr() : nullptr; }
 paro_half_t *half_out(const at::Tensor &t) { return (paro_half_t *)t.data_ptr(); }
@@ -206,10 +217,10 @@ PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (n != 6) { PyErr_SetString(PyExc_TypeError, "rms_norm takes 6 arguments"); return nullptr; }
     const at::Tensor *x = tensor(a[0]), *w = x ? tensor(a[1]) : nullptr, *r;
-    if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*w, at::kHalf, x->size(1))) return nullptr;
+    if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1), *x) || !gpu_vector(*w, at::kHalf, x->size(1), *x)) return nullptr;
     const float eps = (float)PyFloat_AsDouble(a[2]);
     const int64_t T = x->size(0), C = x->size(1);
-    if (PyErr_Occurred() || !maybe(a[3], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    if (PyErr_Occurred() || !maybe(a[3], r) || (r && !gpu_rows(*r, T, C, *x)) || !current(*x)) return nullptr;
     if (!r && a[5] != Py_None) { refuse("H takes the sum with a residual"); return nullptr; }
     at::Tensor y = rows_or_new(a[4], T, C, *x), h;
     if (!y.defined()) return nullptr;
@@ -232,11 +243,11 @@ PyObject *rms_norm_quantize_e4m3(PyObject *, PyObject *const *a, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (n != 6) { PyErr_SetString(PyExc_TypeError, "rms_norm_quantize_e4m3 takes 6 arguments"); return nullptr; }
     const at::Tensor *x = tensor(a[0]), *w = x ? tensor(a[1]) : nullptr, *r;
-    if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*w, at::kHalf, x->size(1))) return nullptr;
+    if (!w || !rows(*x) || !gpu_rows(*x, -1, x->size(1), *x) || !gpu_vector(*w, at::kHalf, x->size(1), *x)) return nullptr;
     const float eps = (float)PyFloat_AsDouble(a[2]);
     int32_t group;
     const int64_t T = x->size(0), C = x->size(1);
-    if (PyErr_Occurred() || !number(a[3], group) || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C))) return nullptr;
+    if (PyErr_Occurred() || !number(a[3], group) || !maybe(a[4], r) || (r && !gpu_rows(*r, T, C, *x)) || !current(*x)) return nullptr;
     if (!r && a[5] != Py_None) { refuse("H takes the sum with a residual"); return nullptr; }
     at::Tensor h;
     if (r && !(h = rows_or_new(a[5], T, C, *x)).defined()) return nullptr;
@@ -260,9 +271,10 @@ PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     if (n != 4) { PyErr_SetString(PyExc_TypeError, "rope takes 4 arguments"); return nullptr; }
-    const paro_rope_t *rp = structure<paro_rope_t>(a[0], g_rope);
+    const RopeOn *on = structure<RopeOn>(a[0], g_rope);
+    const paro_rope_t *rp = on ? &on->c : nullptr;
     const at::Tensor *x = rp ? tensor(a[1]) : nullptr, *at_ = x ? tensor(a[2]) : nullptr;
-    if (!at_ || !rows(*x) || !gpu_rows(*x, -1, x->size(1)) || !gpu_vector(*at_, at::kInt, x->size(0))) return nullptr;
+    if (!at_ || !rows(*x) || !gpu_rows(*x, -1, x->size(1), *x) || !gpu_vector(*at_, at::kInt, x->size(0), *x) || !same_gpu(on->device, *x) || !current(*x)) return nullptr;
     const int64_t T = x->size(0), C = x->size(1);
     if (rp->head_dim <= 0 || C % rp->head_dim) { refuse("rows are not whole heads"); return nullptr; }
     at::Tensor y = rows_or_new(a[3], T, C, *x);
@@ -282,20 +294,22 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     if (n != 8) { PyErr_SetString(PyExc_TypeError, "kv_append takes 8 arguments"); return nullptr; }
-    const paro_kv_cache *c = structure<paro_kv_cache>(a[0], g_cache);
-    const paro_rope_t *rp = !c || a[1] == Py_None ? nullptr : structure<paro_rope_t>(a[1], g_rope);
-    if (!c || (!rp && a[1] != Py_None)) return nullptr;
+    const CacheOn *held = structure<CacheOn>(a[0], g_cache);
+    const RopeOn *on = !held || a[1] == Py_None ? nullptr : structure<RopeOn>(a[1], g_rope);
+    if (!held || (!on && a[1] != Py_None)) return nullptr;
+    const paro_kv_cache *c = &held->c;
+    const paro_rope_t *rp = on ? &on->c : nullptr;
     const at::Tensor *k = tensor(a[2]), *v = k ? tensor(a[3]) : nullptr, *slots = v ? tensor(a[4]) : nullptr, *at_, *q;
     if (!slots || !maybe(a[5], at_) || !maybe(a[6], q)) return nullptr;
     const int64_t width = (int64_t)c->kv_heads * c->head_dim;
-    if (!rows(*k) || !gpu_rows(*k, -1, width) || !gpu_rows(*v, k->size(0), width)) return nullptr;
+    if (!rows(*k) || !gpu_rows(*k, -1, width, *k) || !gpu_rows(*v, k->size(0), width, *k)) return nullptr;
     const int64_t T = k->size(0);
-    if (!gpu_vector(*slots, at::kLong, T) || (at_ && !gpu_vector(*at_, at::kInt, T))) return nullptr;
+    if (!gpu_vector(*slots, at::kLong, T, *k) || (at_ && !gpu_vector(*at_, at::kInt, T, *k))) return nullptr;
+    if (!same_gpu(held->device, *k) || (on && !same_gpu(on->device, *k)) || (q && (!rows(*q) || !gpu_rows(*q, T, q->size(1), *k))) || !current(*k)) return nullptr;
     if (!q && a[7] != Py_None) { refuse("Qr takes rotated queries, and there are none"); return nullptr; }
     at::Tensor out;
     int64_t heads = 0;
     if (q) {
-        if (!rows(*q) || !gpu_rows(*q, T, q->size(1))) return nullptr;
         if (c->head_dim <= 0 || q->size(1) % c->head_dim) { refuse("rows are not whole heads"); return nullptr; }
         heads = q->size(1) / c->head_dim;
         if (!(out = rows_or_new(a[7], T, q->size(1), *q)).defined()) return nullptr;
@@ -318,18 +332,18 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     if (n != 10) { PyErr_SetString(PyExc_TypeError, "paged_attention takes 10 arguments"); return nullptr; }
-    const paro_kv_cache *c = structure<paro_kv_cache>(a[0], g_cache);
+    const CacheOn *held = structure<CacheOn>(a[0], g_cache);
+    const paro_kv_cache *c = held ? &held->c : nullptr;
     const at::Tensor *q = c ? tensor(a[1]) : nullptr, *table = q ? tensor(a[2]) : nullptr, *lengths = table ? tensor(a[3]) : nullptr;
     const at::Tensor *ws = lengths ? tensor(a[4]) : nullptr;
-    if (!ws || !rows(*q) || !gpu_rows(*q, -1, q->size(1))) return nullptr;
+    if (!ws || !rows(*q) || !gpu_rows(*q, -1, q->size(1), *q)) return nullptr;
     const int64_t B = q->size(0);
     if (c->head_dim <= 0 || q->size(1) % c->head_dim) { refuse("rows are not whole heads"); return nullptr; }
-    if (table->scalar_type() != at::kInt || table->dim() != 2 || (table->stride(1) != 1 && table->size(1) != 1) || table->size(0) != B || !table->is_cuda()) {
-        refuse("expected a block table of int32 rows on the GPU, one per sequence");
+    if (table->scalar_type() != at::kInt || table->dim() != 2 || (table->stride(1) != 1 && table->size(1) != 1) || table->size(0) != B) {
+        refuse("expected a block table of int32 rows, one per sequence");
         return nullptr;
     }
-    if (!gpu_vector(*lengths, at::kInt, B)) return nullptr;
-    if (!ws->is_cuda()) { refuse("expected a tensor on the GPU"); return nullptr; }
+    if (!on_gpu(*table, *q) || !gpu_vector(*lengths, at::kInt, B, *q) || !on_gpu(*ws, *q) || !same_gpu(held->device, *q) || !current(*q)) return nullptr;
     const size_t bytes = PyLong_AsSize_t(a[5]);
     const float scale = (float)PyFloat_AsDouble(a[6]);
     int32_t window;

@@ -66,3 +66,24 @@ def test_attention_window_beyond_every_token(P, window):
     o, lse = base._check(P, cache, table, q, rows, lengths, 8, 0.125, window)
     whole, lse_whole = base._check(P, cache, table, q, rows, lengths, 8, 0.125)
     assert (o == whole).all() and (lse == lse_whole).all()
+
+
+def test_frequencies_and_caches_in_host_memory(P):
+    import torch
+    from paper_2511_10645_amd import binding as B_
+    say("frequencies in a tensor of host memory are moved; a cache or frequencies that stay there are refused")
+    f = base._freqs(64)
+    x, pos = torch.randn((3, 128), device="cuda").half(), torch.arange(3, dtype=torch.int32, device="cuda")
+    rope = P.Rope(torch.as_tensor(f), 64)
+    assert rope.inv_freq.is_cuda and (P.paro_rope(rope, x, pos) == P.paro_rope(P.Rope(f, 64), x, pos)).all()
+    there, cache, slots = P.Rope(f, 64, device="cpu"), P.KVCache(2, 2, 64, 16, device="cpu"), torch.arange(3, device="cuda")
+    native = B_._native()
+    try:
+        for B_._host in (native, B_._CtypesCalls):
+            for call in (lambda: P.paro_rope(there, x, pos), lambda: P.paro_kv_append(cache, x, x, slots),
+                         lambda: P.paro_kv_append(P.KVCache(2, 2, 64, 16), x, x, slots, there, pos),
+                         lambda: P.paro_paged_attention(cache, x, torch.zeros((3, 2), dtype=torch.int32, device="cuda"), pos, ws_of(P, cache, 2, 3))):
+                with pytest.raises(AssertionError, match="one GPU"):
+                    call()
+    finally:
+        B_._host = native
