@@ -46,8 +46,8 @@ typedef uint32_t U2 __attribute__((ext_vector_type(2)));
 // waves of a block: two for every SIMD, one where a wave's registers are more than half of them
 template <int D> constexpr int attn_waves() { return D == 256 ? 4 : 8; }
 
-// Blocks for a head of one sequence of `units` units: one where its waves can take a unit each, then at most as many as are joined
-// in one round, and twice that for long ones.
+// Blocks for a head of one sequence of `units` units, if these are few: one where its waves can take a unit each, then at most as many
+// as are joined in one round, and twice that for long ones.
 __host__ __device__ constexpr uint32_t one_parts(uint32_t units, uint32_t waves)
 {
     const uint32_t parts = (units + kLeastUnits - 1) / kLeastUnits, most = units <= 64 ? 8 : 16;
@@ -540,12 +540,14 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     uint32_t share = quotient(total + gridDim.x - 1, gridDim.x, a.per_block), mine = 1;
     if (share < kLeastUnits) share = kLeastUnits;
     // One sequence of some thousand tokens at most: every head begins with a block of its own (segments are numbered `pitch` apart), so that
-    // its parts are as few and as even as can be, and a head of up to WAVES units stays in one block (200 tokens: 9.1 -> 6.2 us).
+    // its parts are as few and as even as can be, and a head of up to WAVES units stays in one block (200 tokens: 9.1 -> 6.5 us).  That ends
+    // at two units a wave: few heads of a longer sequence are spread over all blocks (one of 32768 tokens: 26.5 us in 16 blocks, 12.3 in
+    // 256; a limit of one unit a wave takes 8 heads of 6000 tokens from 13.3 to 14.1).
     const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);
     uint32_t pitch = 0, head_end = total;
     if (a.batch == 1) {
         const uint32_t parts = one_parts(one, WAVES);
-        if (share <= WAVES && hc * parts <= gridDim.x) {
+        if (share <= WAVES && hc * parts <= gridDim.x && one <= 2 * WAVES * parts) {
             const float per_parts = __builtin_amdgcn_rcpf((float)parts);
             share = quotient(one + parts - 1, parts, per_parts);
             pitch = parts * share;

@@ -87,3 +87,26 @@ def test_frequencies_and_caches_in_host_memory(P):
                     call()
     finally:
         B_._host = native
+
+
+def counted(P, cache, hq, B):
+    """A workspace, and a count of the partial results that calls have left in it: the scratch part is 512 of them, the maximum of a
+    part's first query in front, and NaN here until it is written."""
+    import torch
+    total, exchange = P.paro_workspace_bytes_attention(cache, hq, B), P.paro_workspace_exchange_bytes_attention(cache, hq, B)
+    ws = P.Workspace(total)
+    parts = ws.buf[exchange:].view(torch.float32)[:512 * 16 * (cache.head_dim + 4)].view(512, -1)
+    parts.fill_(float("nan"))
+    return ws, lambda: int((~parts[:, 0].isnan()).sum())
+
+
+@pytest.mark.parametrize("n,hkv,D,fmt", [(12000, 1, 128, "fp16"), (32768, 1, 128, "e4m3"), (32768, 2, 64, "fp16"), (16384, 4, 128, "fp16"), (16384, 1, 256, "fp16")])
+def test_attention_of_few_heads_is_spread(P, n, hkv, D, fmt):
+    """One long sequence: a block has two units of 32 tokens for each of its waves (4 with 256 channels, else 8) at most, whatever the
+    number of heads, as long as there are 256 blocks for all."""
+    say(f"attention of {n} tokens of {hkv} heads of {D} {fmt}")
+    case = base._attn(P, [n], 2 * hkv, hkv, D, 16, fmt, n + hkv)
+    ws, count = counted(P, case[0], 2 * hkv, 1)
+    base._check(P, *case, [n], 2 * hkv, D ** -0.5, ws=ws)
+    say(f"  {count()} parts")
+    assert count() >= hkv * n / (32 * 2 * (4 if D == 256 else 8))
