@@ -110,3 +110,41 @@ def test_attention_of_few_heads_is_spread(P, n, hkv, D, fmt):
     base._check(P, *case, [n], 2 * hkv, D ** -0.5, ws=ws)
     say(f"  {count()} parts")
     assert count() >= hkv * n / (32 * 2 * (4 if D == 256 else 8))
+
+
+@pytest.mark.parametrize("lengths,hq,hkv,D,page,fmt,window", [
+    ([40000, 700], 2, 1, 128, 16, "fp16", 0), ([60000], 4, 2, 64, 16, "fp16", 0), ([32768], 8, 4, 128, 32, "fp16", 0), ([32768], 8, 4, 128, 16, "e4m3", 0),
+    ([33000], 20, 1, 128, 16, "e4m3", 0), ([20000], 16, 1, 256, 64, "fp16", 0), ([0, 50001, 1], 3, 1, 64, 16, "e4m3", 40000), ([17000, 17000, 16999], 5, 1, 256, 128, "e4m3", 0)])
+def test_attention_joined_in_two_rounds(P, lengths, hq, hkv, D, page, fmt, window):
+    """More than 32 blocks share a segment: groups of their parts are joined first.  Twice the same, with counters at zero between."""
+    say(f"attention of {lengths}, {hq}/{hkv} x {D}, page {page} {fmt}, window {window}")
+    case = base._attn(P, lengths, hq, hkv, D, page, fmt, sum(lengths), spread=1.5)
+    ws, count = counted(P, case[0], hq, len(lengths))
+    o, lse = base._check(P, *case, lengths, hq, D ** -0.5, window, ws=ws)
+    segments = hkv * -(-hq // hkv // 16) * sum(n > 10000 for n in lengths)
+    say(f"  {count()} parts of {segments} long segments")
+    assert count() > 33 * segments + 2 * len(lengths)
+    again, lse2 = base._check(P, *case, lengths, hq, D ** -0.5, window, ws=ws)
+    assert (o == again).all() and (lse == lse2).all()
+
+
+def test_attention_joined_in_two_rounds_replayed(P):
+    import torch
+    say("a captured call of 33 and more parts a head, replayed with other queries and lengths")
+    case = base._attn(P, [33000], 8, 2, 64, 16, "fp16", 6)
+    cache, table, q, rows = case
+    ws, count = counted(P, cache, 8, 1)
+    x, ln, tb = cuda(q).clone(), cuda(np.array([33000], np.int32)), cuda(table)
+    P.paro_paged_attention(cache, x, tb, ln, ws)
+    assert count() > 2 * 33
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out, lse = P.paro_paged_attention(cache, x, tb, ln, ws, with_lse=True)
+    for n in (33000, 20000, 500, 33000):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        ln.fill_(n)
+        want, l_want = P.paro_paged_attention(cache, x, tb, ln, ws_of(P, cache, 8, 1), with_lse=True)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert (out == want).all() and (lse == l_want).all()
