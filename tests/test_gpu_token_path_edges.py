@@ -148,3 +148,41 @@ def test_attention_joined_in_two_rounds_replayed(P):
         g.replay()
         torch.cuda.synchronize()
         assert (out == want).all() and (lse == l_want).all()
+
+
+@pytest.mark.parametrize("D,hq,hkv", [(64, 3, 1), (128, 4, 2), (256, 2, 1)])
+def test_attention_over_all_of_e4m3(P, D, hq, hkv):
+    """Every code at every scale that the append writes, from fp16's subnormals to 240 * 2^8: in sequences of one token, whose result is
+    its value, and of 48 tokens of one scale."""
+    import torch
+    say(f"attention over every E4M3 value, {hq}/{hkv} x {D}")
+    rs = np.random.default_rng(D)
+    scales, page = np.arange(112, 136, dtype=np.uint8), 16
+    n_pages = 5 * len(scales)
+    codes = rs.integers(0, 256, (2, n_pages, hkv, page, D)).astype(np.uint8)
+    s = np.broadcast_to(np.repeat(scales, 5)[:, None, None], (n_pages, hkv, page))
+    most = np.where(s == 135, 0x77, 0x7e)[..., None]                    # 240 and 448
+    codes = (codes & 128 | np.minimum(codes & 127, most)).astype(np.uint8)
+    assert all(len(np.unique(codes[1, i:i + 5])) == (254 if i < n_pages - 5 else 240) for i in range(0, n_pages, 5))
+    k = np.ascontiguousarray(codes[0].reshape(n_pages, hkv, page, D // 16, 16).transpose(0, 1, 3, 2, 4))
+    cache = P.KVCache.from_device(cuda(k), cuda(codes[1]), cuda(s.copy()), cuda(s.copy()))
+    q = (rs.standard_normal((2 * len(scales), hq * D)) * 0.01).astype(np.float16)
+    table = np.zeros((2 * len(scales), 3), np.int32)
+    table[::2, 0] = np.arange(0, n_pages, 5)
+    table[1::2] = np.arange(0, n_pages, 5)[:, None] + [1, 2, 3]
+    lengths = [1, 48] * len(scales)
+    rows = [ref.cache_rows(cache, table[i, np.arange(n) // page].astype(np.int64) * page + np.arange(n) % page) for i, n in enumerate(lengths)]
+    o, lse = base._check(P, cache, table, q, rows, lengths, hq, 2.0 ** -8)
+    one = np.stack([rows[i][1][0] for i in range(0, len(lengths), 2)]).repeat(hq // hkv, axis=1)
+    assert np.array_equal(o[::2].cpu().numpy().reshape(one.shape).astype(np.float64), one)
+    # and rows that the append itself puts at these scales
+    x = np.zeros((48, hkv, D))
+    x[:] = rs.uniform(-1, 1, x.shape) * 2.0 ** np.linspace(-20, 15.9, 48)[:, None, None]
+    x[0], x[1, :, ::2], x[2, :, 0] = 65504, -65504, 2.0 ** -24
+    x = cuda(x.reshape(48, -1).astype(np.float16))
+    cache = P.KVCache(3, hkv, D, page, "e4m3")
+    P.paro_kv_append(cache, x, x, cuda(np.arange(48, dtype=np.int64)))
+    held = ref.cache_rows(cache, np.arange(48))
+    assert np.abs(held[1]).max() == 61440 and {int(b) for b in cache.v_scale.unique()} >= set(range(114, 136))
+    for n in (1, 2, 3, 20, 48):
+        base._check(P, cache, np.arange(3, dtype=np.int32)[None], q[:1], [(held[0][:n], held[1][:n])], [n], hq, 2.0 ** -10)
