@@ -428,8 +428,9 @@ paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rope_t *rope, 
  * table's end; tokens of a page the cache does not have are left out.  Cache places past n do not matter,
  * whatever they hold.  lse (NULL: not wanted): fp32 [batch][q_heads], ln sum_t exp(scale q . k_t).
  * Q, O: fp16 rows of q_heads heads of head_dim, O nowhere in Q (PARO_ERR_SHAPE where O is Q); q_heads a multiple of kv_heads (16 of them share one reading of their
- * key-value head).  scale must be finite.  A key or value that is not finite makes its heads' results not finite, unless
- * its score is -inf.  table_width * page at most 2^30, as are the units of 32 tokens of all heads.
+ * key-value head).  scale must be finite.  A key that is not finite makes its heads' results not finite, unless its score
+ * is -inf, which gives its token the weight 0.  A value that is not finite makes its channel's results not finite whatever its
+ * token's weight, 0 among them.  table_width * page at most 2^30, as are the units of 32 tokens of all heads.
  * ws: >= paro_workspace_bytes_attention() bytes, 256-byte aligned, in the two parts described at
  * paro_workspace_bytes(): the exchange part (paro_workspace_exchange_bytes_attention(), zero-filled once,
  * all zero again after every call) counts arrivals, the scratch part at the buffer's end holds fp32 partial

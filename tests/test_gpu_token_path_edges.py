@@ -186,3 +186,30 @@ def test_attention_over_all_of_e4m3(P, D, hq, hkv):
     assert np.abs(held[1]).max() == 61440 and {int(b) for b in cache.v_scale.unique()} >= set(range(114, 136))
     for n in (1, 2, 3, 20, 48):
         base._check(P, cache, np.arange(3, dtype=np.int32)[None], q[:1], [(held[0][:n], held[1][:n])], [n], hq, 2.0 ** -10)
+
+
+def test_attention_values_at_scores_of_minus_infinity(P):
+    """A key that is not there for a query (score -inf) may hold anything else; its value has to be finite, for 0 * NaN is NaN.  Values past
+    the end or on pages that are not there do not matter."""
+    import torch
+    say("attention: values that are not finite, at scores of -inf and in places that are left out")
+    cache, table, q, rows = base._attn(P, [40], 2, 1, 64, 16, "fp16", 4)
+    q = np.abs(q)
+    cache.k[table[0, 0], 0, 0, 5, 0] = float("-inf")
+    at = np.r_[0:5, 6:40]
+    for value in (3.0, float("nan"), float("inf")):
+        cache.v[table[0, 0], 0, 5] = value
+        o, lse = P.paro_paged_attention(cache, cuda(q), cuda(table), cuda(np.array([40], np.int32)), ws_of(P, cache, 2, 1), 0.125, with_lse=True)
+        w = ref.attention(q[0].reshape(2, 64), rows[0][0][at], rows[0][1][at], 0.125)
+        within(lse.cpu().numpy()[0], w[1], w[3], "lse")
+        if value == 3.0:
+            within(o.cpu().numpy().reshape(2, 64), w[0], w[2], "o")
+        else:
+            assert bool(o.isnan().all())
+    o = P.paro_paged_attention(cache, cuda(q), cuda(table), cuda(np.array([5], np.int32)), ws_of(P, cache, 2, 1), 0.125)
+    assert bool(torch.isfinite(o).all())
+    gone = table.copy()
+    gone[0, 0] = -1
+    o = P.paro_paged_attention(cache, cuda(q), cuda(gone), cuda(np.array([40], np.int32)), ws_of(P, cache, 2, 1), 0.125)
+    w = ref.attention(q[0].reshape(2, 64), rows[0][0][16:], rows[0][1][16:], 0.125)
+    within(o.cpu().numpy().reshape(2, 64), w[0], w[2], "without the page")
