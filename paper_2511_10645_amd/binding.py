@@ -759,9 +759,6 @@ class Rope:
         self.inv_freq, self.head_dim, self.rot_dim = inv_freq, head_dim, 2 * inv_freq.shape[0]
         self.c = _CRope(head_dim, self.rot_dim, ROPE_LAYOUTS[layout], magnitude, _ptr(inv_freq), _device_of(inv_freq))
 
-    def ref(self):
-        return ctypes.byref(self.c)
-
 
 def paro_rope(rope: Rope, X: torch.Tensor, positions: torch.Tensor, Y: torch.Tensor | None = None) -> torch.Tensor:
     """Rows of heads rotated to int32 positions [T]; Y may be X."""
