@@ -13,7 +13,7 @@
 
 namespace {
 
-// The ctypes classes of the two structures (binding.py hands them over once).
+// The ctypes classes of the structures (binding.py hands them over once).
 PyObject *g_rotation, *g_weight, *g_rope, *g_cache;
 
 // A ctypes structure of class `type` through the buffer protocol; NULL with an exception set if it is anything else.

@@ -37,7 +37,7 @@ constexpr float kPShift = 15.0f;                 // p is held 2^15 times
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRsrcRaw = 0x00020000;             // raw buffer, 32-bit data format
 constexpr int kAgent = 16;                       // agent scope: past the L2 of the XCD
-constexpr int kOnce = 2;                         // keys and values are read once: non-temporal (131071 tokens: 90 us, 98 without)
+constexpr int kOnce = 2;                         // keys and values are read once: non-temporal (131071 tokens from memory: 90 us, 98 without)
 
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
@@ -347,7 +347,8 @@ __device__ inline void take_in(Running<D> &st, const float (&x)[8], const Values
 
 __device__ inline float lse_of(float m, float sum) { return sum == 0.0f ? -INFINITY : (m - kPShift + __builtin_amdgcn_logf(sum)) * kLn2; }
 
-// x / d for a quotient up to 2^20, inv = 1 / d to some units of fp32.
+// x / d for a quotient up to 2^20, inv = 1 / d to some units of fp32; up to 2^22 with an exact inv (units of a block: above 2^20 only
+// where the grid is at its 256 blocks).
 __device__ inline uint32_t quotient(uint32_t x, uint32_t d, float inv)
 {
     const uint32_t q = (uint32_t)((float)x * inv), r = x - q * d;        // off by one at most
@@ -540,7 +541,7 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     uint32_t share = quotient(total + gridDim.x - 1, gridDim.x, a.per_block), mine = 1;
     if (share < kLeastUnits) share = kLeastUnits;
     // One sequence of some thousand tokens at most: every head begins with a block of its own (segments are numbered `pitch` apart), so that
-    // its parts are as few and as even as can be, and a head of up to WAVES units stays in one block (200 tokens: 9.1 -> 6.5 us).  That ends
+    // its parts are as few and as even as can be, and a head of up to WAVES units stays in one block (200 tokens: 9.1 -> 6.8 us).  That ends
     // at two units a wave: few heads of a longer sequence are spread over all blocks (one of 32768 tokens: 26.5 us in 16 blocks, 12.3 in
     // 256; a limit of one unit a wave takes 8 heads of 6000 tokens from 13.3 to 14.1).
     const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)upto, 0);
