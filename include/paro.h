@@ -394,13 +394,18 @@ paro_status paro_rope(const paro_rope_t *rope, const paro_half_t *X, int64_t ldx
  *   format 1: E4M3 codes, k [n_pages][kv_heads][head_dim/16][page][16], v [n_pages][kv_heads][page][head_dim],
  *             and one scale byte per token and head, k_scale / v_scale [n_pages][kv_heads][page]: the code's
  *             value counts 2^(byte - 127) times.  paro_kv_append writes bytes 112 to 135; with those of a caller's
- *             own outside, values that fp16 does not have are rounded or infinite */
+ *             own outside, values that fp16 does not have are rounded or infinite
+ *   format 4: MXFP4, E2M1 codes (those of paro_rotate_scale_quantize_mxfp4, channel 2i in the low half of byte i), k
+ *             [n_pages][kv_heads][head_dim/32][page][16], v [n_pages][kv_heads][page][head_dim/2], and one scale byte per
+ *             token, head and 32 channels, k_scale / v_scale [n_pages][kv_heads][head_dim/32][page]: the codes' values count
+ *             2^(byte - 127) times, 255: they are NaN.  paro_kv_append writes bytes 104 to 140 and 255; with those of a
+ *             caller's own outside, values that fp16 does not have are rounded or infinite */
 typedef struct {
     int32_t n_pages;
     int32_t page;             /* tokens of a page: a power of two, 16..1024                     */
     int32_t kv_heads;
     int32_t head_dim;         /* 64, 128 or 256                                                 */
-    int32_t format;           /* 0: fp16, 1: E4M3                                               */
+    int32_t format;           /* 0: fp16, 1: E4M3, 4: MXFP4                                     */
     void *k, *v;              /* device, 16-byte aligned                                        */
     uint8_t *k_scale, *v_scale; /* device, 4-byte aligned; NULL for format 0                     */
 } paro_kv_cache;
@@ -413,7 +418,10 @@ typedef struct {
  * Format 1: every (token, head) row takes the scale 2^e, the least e in -15..8 with max|row| <= 448 * 2^e, of the
  * unrounded rotated row, and codes row / 2^e rounded to nearest even, those of e = 8 kept within 240 (larger
  * ones would stand for values that fp16 does not have); values that are not finite become the NaN code and
- * do not count for e.  All values a format-1 cache written by this call stands for are fp16 values.  No workspace. */
+ * do not count for e.  All values a format-1 cache written by this call stands for are fp16 values.
+ * Format 4: every 32 channels of a (token, head) row take the scale 2^e, e = floor(log2 max|v|) - 2 kept within -23..13, of the
+ * unrounded rotated values, and codes v / 2^e rounded to nearest, halves to the even code, saturating at 6; 32 channels one
+ * of which is not finite are NaN (scale byte 255).  All other values are fp16 values here too.  No workspace. */
 paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rope_t *rope, const paro_half_t *K, int64_t ldk,
                            const paro_half_t *V, int64_t ldv, const int64_t *slots, const int32_t *positions,
                            int32_t T, const paro_half_t *Q, int64_t ldq, int32_t q_heads, paro_half_t *Qr,
@@ -443,6 +451,45 @@ paro_status paro_paged_attention(const paro_kv_cache *cache, const paro_half_t *
                                  const int32_t *lengths, int32_t batch, float scale, int32_t window,
                                  paro_half_t *O, int64_t ldo, float *lse, void *ws, size_t ws_bytes,
                                  void *stream);
+
+/* The same with other scores: in place of x = scale q_h . k_t the softmax and lse take
+ *      x = cap tanh(scale q_h . k_t / cap) - slopes[h] |p - t|
+ * for a query at position p (here p = n - 1): scores that stay within +-cap, a bias that grows with the distance, or both.
+ * A score of -inf is -cap under a cap, and its token counts.  cap: 0 (none) or positive, finite, with scale / cap finite
+ * (PARO_ERR_SHAPE otherwise).  slopes: device fp32 [q_heads], 4-byte aligned, or NULL (none); finite values.  tanh is off by
+ * 2^-22 of itself at most.  scores NULL, or with neither: paro_paged_attention. */
+typedef struct {
+    float cap;
+    const float *slopes;
+} paro_scores_t;
+paro_status paro_paged_attention_scored(const paro_kv_cache *cache, const paro_half_t *Q, int64_t ldq, int32_t q_heads,
+                                        const int32_t *block_table, int64_t ld_table, int32_t table_width,
+                                        const int32_t *lengths, int32_t batch, float scale, int32_t window,
+                                        const paro_scores_t *scores, paro_half_t *O, int64_t ldo, float *lse,
+                                        void *ws, size_t ws_bytes, void *stream);
+
+/* Attention of the new tokens of each of `batch` sequences, any number of them each (a prompt, a piece of one, a few drafts), over the
+ * sequence's cached tokens, the new ones among them.  The rows of sequence b are starts[b] .. starts[b+1] - 1 of Q and O, its newest
+ * tokens: the last of its m rows is at position n - 1, n = lengths[b], row i at p = n - m + i.  A row attends to the tokens t with
+ *      max(0, p - window + 1, first) <= t <= p   (window 0: from 0 on),   and from the same t on to all t < prefix
+ * prefix: device [batch], tokens of the sequence's begin that its rows see from both sides (at most n count), or NULL; first: device [T], the first token
+ * of each row's document, where several lie in one sequence, or NULL.
+ * Otherwise as paro_paged_attention_scored, with one row of O (and of lse, fp32 [T][q_heads]) per row of Q: cache formats, block table, missing pages,
+ * rows with nothing to attend to (also those at p < 0), scores, scale.  A value that is not finite makes its channel's results not finite
+ * for the rows that attend to its token, whatever the weight, and for no others.  Weights of the softmax are rounded to fp16 (2^-11) for the product with
+ * the values, which paro_paged_attention does not.
+ * starts: device [batch + 1], from 0 to T and not falling (rows outside them are left as they were; values out of range are taken as 0 or T, and rows that two
+ * sequences claim hold either's results).  T at most 2^24, T * q_heads at most 2^30, table_width * page at most 2^30.  O nowhere in Q.
+ * ws: >= paro_workspace_bytes_prompt() bytes, 256-byte aligned, in the two parts described at paro_workspace_bytes(); as with
+ * paro_paged_attention, counters in the exchange part are zero again after every call, and blocks never wait for each other. */
+size_t paro_workspace_exchange_bytes_prompt(const paro_kv_cache *cache, int32_t q_heads, int32_t T, int32_t batch);
+size_t paro_workspace_bytes_prompt(const paro_kv_cache *cache, int32_t q_heads, int32_t T, int32_t batch);
+paro_status paro_prompt_attention(const paro_kv_cache *cache, const paro_half_t *Q, int64_t ldq, int32_t q_heads,
+                                  int32_t T, const int32_t *starts, const int32_t *block_table, int64_t ld_table,
+                                  int32_t table_width, const int32_t *lengths, int32_t batch, float scale,
+                                  int32_t window, const paro_scores_t *scores, const int32_t *prefix,
+                                  const int32_t *first, paro_half_t *O, int64_t ldo, float *lse, void *ws,
+                                  size_t ws_bytes, void *stream);
 
 /* Test hooks for the bit-exact gate --------------------------------------------------- */
 

@@ -61,6 +61,10 @@ class _CKVCache(ctypes.Structure):
     ]
 
 
+class _CScores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -129,6 +133,13 @@ def lib():
         L.paro_workspace_bytes_attention.restype = sz
         L.paro_workspace_bytes_attention.argtypes = [cp, i32, i32]
         L.paro_paged_attention.argtypes = [cp, vp, i64, i32, vp, i64, i32, vp, i32, f32, i32, vp, i64, vp, vp, sz, vp]
+        sp = ctypes.POINTER(_CScores)
+        L.paro_paged_attention_scored.argtypes = [cp, vp, i64, i32, vp, i64, i32, vp, i32, f32, i32, sp, vp, i64, vp, vp, sz, vp]
+        L.paro_workspace_exchange_bytes_prompt.restype = sz
+        L.paro_workspace_exchange_bytes_prompt.argtypes = [cp, i32, i32, i32]
+        L.paro_workspace_bytes_prompt.restype = sz
+        L.paro_workspace_bytes_prompt.argtypes = [cp, i32, i32, i32]
+        L.paro_prompt_attention.argtypes = [cp, vp, i64, i32, i32, vp, vp, i64, i32, vp, i32, f32, i32, sp, vp, vp, vp, i64, vp, vp, sz, vp]
         L.paro_diag_read_stream.argtypes = [vp, sz, vp, i32, vp]
         L.paro_diag_mfma_f16.argtypes = [vp, sz, i32, i32, i32, vp]
         L.paro_diag_mfma_f16_flops.argtypes = [i32, i32]
@@ -143,7 +154,8 @@ def lib():
                      "paro_rotate_scale_quantize_int4", "paro_rotate_scale_quantize_mxfp4",
                      "paro_diag_read_stream", "paro_diag_mfma_f16", "paro_fwht", "paro_mxfp4_quantize_weight",
                      "paro_mxfp4_repack", "paro_mxfp4_unpack", "paro_mxfp4_linear", "paro_rotated_linear_mxfp4", "paro_rms_norm",
-                     "paro_rms_norm_quantize_e4m3", "paro_rope_frequencies_host", "paro_rope", "paro_kv_append", "paro_paged_attention"):
+                     "paro_rms_norm_quantize_e4m3", "paro_rope_frequencies_host", "paro_rope", "paro_kv_append", "paro_paged_attention",
+                     "paro_paged_attention_scored", "paro_prompt_attention"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -238,24 +250,32 @@ class _CtypesCalls:
         return Qr if st == PARO_OK else st
 
     @staticmethod
-    def paged_attention(cache, Q, table, lengths, buf, nbytes, scale, window, O, with_lse):
-        ldq = _gpu_rows(Q)
-        B = Q.shape[0]
-        assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
-        assert table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.shape[0] == B
-        _gpu_vector(lengths, torch.int32, B, Q)
-        assert table.is_cuda and buf.is_cuda, "expected a tensor on the GPU"
-        for device in (table.device.index, buf.device.index, cache.device):
-            _same_gpu(device, Q)
-        _current(Q)
-        assert table.shape[1] < 2 ** 31
-        _number(window)
-        heads = Q.shape[1] // cache.head_dim
+    def paged_attention(cache, Q, table, lengths, buf, nbytes, scale, window, O, with_lse, cap=0.0, slopes=None):
+        ldq, B = _gpu_rows(Q), Q.shape[0]
+        heads = _attention_inputs(cache, Q, table, lengths, buf, window, B)
+        scores = _scores(cap, slopes, heads, Q)
         O, ldo = _rows_or_new(O, B, Q.shape[1], Q)
         lse = torch.empty((B, heads), dtype=torch.float32, device=Q.device) if with_lse else None
-        st = lib().paro_paged_attention(ctypes.byref(cache), Q.data_ptr(), ldq, heads, table.data_ptr(), table.shape[1] if B == 1 else table.stride(0),
-                                        table.shape[1], lengths.data_ptr(), B, scale, window, O.data_ptr(), ldo, _ptr(lse), buf.data_ptr(), nbytes,
-                                        _stream())
+        st = lib().paro_paged_attention_scored(ctypes.byref(cache), Q.data_ptr(), ldq, heads, table.data_ptr(), table.shape[1] if B == 1 else table.stride(0),
+                                               table.shape[1], lengths.data_ptr(), B, scale, window, scores, O.data_ptr(), ldo, _ptr(lse), buf.data_ptr(),
+                                               nbytes, _stream())
+        return st if st != PARO_OK else (O, lse) if with_lse else O
+
+    @staticmethod
+    def prompt_attention(cache, Q, starts, table, lengths, buf, nbytes, scale, window, cap, slopes, prefix, first, O, with_lse):
+        ldq, T, B = _gpu_rows(Q), Q.shape[0], table.shape[0]
+        heads = _attention_inputs(cache, Q, table, lengths, buf, window, B)
+        _gpu_vector(starts, torch.int32, B + 1, Q)
+        if prefix is not None:
+            _gpu_vector(prefix, torch.int32, B, Q)
+        if first is not None:
+            _gpu_vector(first, torch.int32, T, Q)
+        scores = _scores(cap, slopes, heads, Q)
+        O, ldo = _rows_or_new(O, T, Q.shape[1], Q)
+        lse = torch.empty((T, heads), dtype=torch.float32, device=Q.device) if with_lse else None
+        st = lib().paro_prompt_attention(ctypes.byref(cache), Q.data_ptr(), ldq, heads, T, starts.data_ptr(), table.data_ptr(),
+                                         table.shape[1] if B == 1 else table.stride(0), table.shape[1], lengths.data_ptr(), B, scale, window, scores,
+                                         _ptr(prefix), _ptr(first), O.data_ptr(), ldo, _ptr(lse), buf.data_ptr(), nbytes, _stream())
         return st if st != PARO_OK else (O, lse) if with_lse else O
 
 
@@ -269,6 +289,7 @@ def _native():
             from . import paro_host
             paro_host.types(_CRotation, _CW4Weight)
             paro_host.token_types(_CRope, _CKVCache)
+            paro_host.prompt_attention  # noqa: B018
             _host = paro_host
         except (ImportError, AttributeError) as e:      # not built, or built against another torch or for other calls
             if os.path.exists(_HOST_PATH):
@@ -439,9 +460,9 @@ class Workspace:
         return hi <= lo or int(self.buf[lo:hi].max().item()) == 0
 
     @classmethod
-    def shared(cls, calls, device="cuda", attention=()):
+    def shared(cls, calls, device="cuda", attention=(), prompts=()):
         """One workspace for calls of several shapes: calls = [(rot or None, weight, T), ...], attention = [(cache, q_heads,
-        batch), ...].  Sized as the largest exchange part plus the largest scratch part, so no call's scratch touches
+        batch), ...], prompts = [(cache, q_heads, T, batch), ...] (which serves fewer rows and sequences too).  Sized as the largest exchange part plus the largest scratch part, so no call's scratch touches
         another's exchange part."""
         ex = sc = 0
         for rot, w, T in calls:
@@ -449,6 +470,9 @@ class Workspace:
             ex, sc = max(ex, e), max(sc, total - e)
         for call in attention:
             total, e = paro_workspace_bytes_attention(*call), paro_workspace_exchange_bytes_attention(*call)
+            ex, sc = max(ex, e), max(sc, total - e)
+        for call in prompts:
+            total, e = paro_workspace_bytes_prompt(*call), paro_workspace_exchange_bytes_prompt(*call)
             ex, sc = max(ex, e), max(sc, total - e)
         ws = cls(ex + sc, device)
         ws.exchange_bytes = ex
@@ -534,6 +558,26 @@ def _device_of(*tensors) -> int:
 
 def _number(n: int) -> None:
     assert -2 ** 31 <= n < 2 ** 31, "a number beyond 32 bits"
+
+
+def _attention_inputs(cache, Q, table, lengths, buf, window: int, B: int) -> int:
+    """The query heads of an attention call over `B` sequences, once its tensors are what it takes."""
+    assert Q.shape[1] % cache.head_dim == 0, "rows are not whole heads"
+    assert table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.shape[0] == B
+    _gpu_vector(lengths, torch.int32, B, Q)
+    assert table.is_cuda and buf.is_cuda, "expected a tensor on the GPU"
+    for device in (table.device.index, buf.device.index, cache.device):
+        _same_gpu(device, Q)
+    _current(Q)
+    assert table.shape[1] < 2 ** 31 and B < 2 ** 31
+    _number(window)
+    return Q.shape[1] // cache.head_dim
+
+
+def _scores(cap: float, slopes, heads: int, like: torch.Tensor):
+    if slopes is not None:
+        _gpu_vector(slopes, torch.float32, heads, like)
+    return ctypes.byref(_CScores(cap, _ptr(slopes)))
 
 
 def _rows_or_new(x, T: int, width: int, like: torch.Tensor):
@@ -765,37 +809,44 @@ def paro_rope(rope: Rope, X: torch.Tensor, positions: torch.Tensor, Y: torch.Ten
     return _output((_host or _native()).rope(rope.c, X, positions, Y), "paro_rope")
 
 
+KV_FORMATS = {"fp16": 0, "e4m3": 1, "mxfp4": 4}
+
+
 class KVCache:
-    """A paged key-value cache on the device (struct paro_kv_cache), "fp16" or "e4m3".  Keys: [n_pages][kv_heads][head_dim/u][page][u], u the
-    channels of 16 bytes; values [n_pages][kv_heads][page][head_dim]; e4m3 adds scale bytes [n_pages][kv_heads][page] to either."""
+    """A paged key-value cache on the device (struct paro_kv_cache), "fp16", "e4m3" or "mxfp4".  Keys: [n_pages][kv_heads][units][page][16 bytes], a unit
+    being the channels of 16 bytes (8, 16 or 32); values [n_pages][kv_heads][page][head_dim], two channels to a byte in mxfp4; e4m3 adds scale bytes
+    [n_pages][kv_heads][page] to either, mxfp4 [n_pages][kv_heads][head_dim/32][page]."""
 
     def __init__(self, n_pages: int, kv_heads: int, head_dim: int, page: int = 16, format: str = "fp16", device="cuda"):
-        dtype, u = {"fp16": (torch.float16, 8), "e4m3": (torch.uint8, 16)}[format]
-        k = torch.zeros((n_pages, kv_heads, head_dim // u, page, u), dtype=dtype, device=device)
-        v = torch.zeros((n_pages, kv_heads, page, head_dim), dtype=dtype, device=device)
-        scales = [torch.full((n_pages, kv_heads, page), 127, dtype=torch.uint8, device=device) for _ in range(2)] if u == 16 else (None, None)
+        dtype, u, held = {"fp16": (torch.float16, 8, 1), "e4m3": (torch.uint8, 16, 1), "mxfp4": (torch.uint8, 16, 2)}[format]
+        k = torch.zeros((n_pages, kv_heads, head_dim // held // u, page, u), dtype=dtype, device=device)
+        v = torch.zeros((n_pages, kv_heads, page, head_dim // held), dtype=dtype, device=device)
+        rows = (n_pages, kv_heads, head_dim // 32, page) if format == "mxfp4" else (n_pages, kv_heads, page)
+        scales = [torch.full(rows, 127, dtype=torch.uint8, device=device) for _ in range(2)] if u == 16 else (None, None)
         self._take(k, v, *scales)
 
     @classmethod
     def from_device(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
-        """Wrap tensors in the cache's layout that already live on the device."""
+        """Wrap tensors in the cache's layout that already live on the device (scales of four dimensions: mxfp4, of three: e4m3, none: fp16)."""
         self = cls.__new__(cls)
         self._take(k, v, k_scale, v_scale)
         return self
 
     def _take(self, k, v, k_scale, v_scale):
         assert (k_scale is None) == (v_scale is None), "scales of both keys and values, or of neither"
-        e4m3 = k_scale is not None
-        self.n_pages, self.kv_heads, self.page, self.head_dim = v.shape
-        u = 16 if e4m3 else 8
-        assert k.dtype == v.dtype == (torch.uint8 if e4m3 else torch.float16) and k.is_contiguous() and v.is_contiguous()
-        assert k.shape == (self.n_pages, self.kv_heads, self.head_dim // u, self.page, u)
-        for s in (k_scale, v_scale) if e4m3 else ():
-            assert s.dtype == torch.uint8 and s.is_contiguous() and s.shape == (self.n_pages, self.kv_heads, self.page)
-        self.format = "e4m3" if e4m3 else "fp16"
+        scaled = k_scale is not None
+        self.format = "fp16" if not scaled else "mxfp4" if k_scale.dim() == 4 else "e4m3"
+        self.n_pages, self.kv_heads, self.page, width = v.shape
+        self.head_dim = 2 * width if self.format == "mxfp4" else width
+        u = 16 if scaled else 8
+        assert k.dtype == v.dtype == (torch.uint8 if scaled else torch.float16) and k.is_contiguous() and v.is_contiguous()
+        assert k.shape == (self.n_pages, self.kv_heads, width // u, self.page, u)
+        rows = (self.n_pages, self.kv_heads, self.head_dim // 32, self.page) if self.format == "mxfp4" else (self.n_pages, self.kv_heads, self.page)
+        for s in (k_scale, v_scale) if scaled else ():
+            assert s.dtype == torch.uint8 and s.is_contiguous() and s.shape == rows
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.c = _CKVCache(self.n_pages, self.page, self.kv_heads, self.head_dim, int(e4m3), _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale),
-                         _device_of(k, v, *((k_scale, v_scale) if e4m3 else ())))
+        self.c = _CKVCache(self.n_pages, self.page, self.kv_heads, self.head_dim, KV_FORMATS[self.format], _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale),
+                         _device_of(k, v, *((k_scale, v_scale) if scaled else ())))
 
     def ref(self):
         return ctypes.byref(self.c)
@@ -816,9 +867,34 @@ def paro_workspace_exchange_bytes_attention(cache: KVCache, q_heads: int, batch:
 
 
 def paro_paged_attention(cache: KVCache, Q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, ws: Workspace,
-                         scale: float | None = None, window: int = 0, O: torch.Tensor | None = None, with_lse: bool = False):
-    """One new token of every sequence against its cached ones (int32 block_table [B][pages], lengths [B]): O, or (O, lse fp32 [B][q_heads])."""
+                         scale: float | None = None, window: int = 0, O: torch.Tensor | None = None, with_lse: bool = False, cap: float = 0.0,
+                         slopes: torch.Tensor | None = None):
+    """One new token of every sequence against its cached ones (int32 block_table [B][pages], lengths [B]): O, or (O, lse fp32 [B][q_heads]).
+    cap: scores become cap * tanh(score / cap); slopes (fp32 [q_heads]): and are lowered by slope * distance."""
     if scale is None:
         scale = cache.head_dim ** -0.5
-    return _output((_host or _native()).paged_attention(cache.c, Q, block_table, lengths, ws.buf, ws.nbytes, scale, window, O, with_lse),
-                   "paro_paged_attention")
+    if cap == 0 and slopes is None:
+        return _output((_host or _native()).paged_attention(cache.c, Q, block_table, lengths, ws.buf, ws.nbytes, scale, window, O, with_lse),
+                       "paro_paged_attention")
+    return _output((_host or _native()).paged_attention(cache.c, Q, block_table, lengths, ws.buf, ws.nbytes, scale, window, O, with_lse, cap, slopes),
+                   "paro_paged_attention_scored")
+
+
+def paro_workspace_bytes_prompt(cache: KVCache, q_heads: int, T: int, batch: int) -> int:
+    return lib().paro_workspace_bytes_prompt(cache.ref(), q_heads, T, batch)
+
+
+def paro_workspace_exchange_bytes_prompt(cache: KVCache, q_heads: int, T: int, batch: int) -> int:
+    return lib().paro_workspace_exchange_bytes_prompt(cache.ref(), q_heads, T, batch)
+
+
+def paro_prompt_attention(cache: KVCache, Q: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor, ws: Workspace,
+                          scale: float | None = None, window: int = 0, cap: float = 0.0, slopes: torch.Tensor | None = None,
+                          prefix: torch.Tensor | None = None, first: torch.Tensor | None = None, O: torch.Tensor | None = None, with_lse: bool = False):
+    """The newest tokens of every sequence, rows starts[b] .. starts[b+1] - 1 of Q (int32 starts [B+1]), against its cached ones, themselves among them
+    (block_table, lengths, scale, cap and slopes as for one token): O, or (O, lse fp32 [T][q_heads]).  A row sees the tokens up to its own, within the
+    window, from `first` on (int32 [T]: where its document begins), and from there on also all below `prefix` (int32 [B])."""
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    return _output((_host or _native()).prompt_attention(cache.c, Q, starts, block_table, lengths, ws.buf, ws.nbytes, scale, window, cap, slopes, prefix,
+                                                         first, O, with_lse), "paro_prompt_attention")

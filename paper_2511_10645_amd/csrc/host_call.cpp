@@ -327,43 +327,104 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// paged_attention(cache, Q, block_table, lengths, workspace, bytes, scale, window, O or None, with_lse) -> O, or (O, lse)
+// What both attentions take besides their rows: cache, block table, lengths, workspace, scale, window and scores.
+struct Attention {
+    const paro_kv_cache *c;
+    const at::Tensor *q, *table, *lengths, *ws, *slopes;
+    int64_t batch, heads, ld;
+    size_t bytes;
+    float scale;
+    int32_t window;
+    paro_scores_t scores;
+
+    // false with an exception set; batch < 0: as many sequences as rows
+    bool take(PyObject *cache, PyObject *Q, PyObject *block_table, PyObject *lens, PyObject *workspace, PyObject *nbytes, PyObject *scale_, PyObject *window_,
+              PyObject *cap, PyObject *slopes_, bool row_each)
+    {
+        const CacheOn *held = structure<CacheOn>(cache, g_cache);
+        c = held ? &held->c : nullptr;
+        q = c ? tensor(Q) : nullptr;
+        table = q ? tensor(block_table) : nullptr;
+        lengths = table ? tensor(lens) : nullptr;
+        ws = lengths ? tensor(workspace) : nullptr;
+        if (!ws || !rows(*q) || !gpu_rows(*q, -1, q->size(1), *q)) return false;
+        if (c->head_dim <= 0 || q->size(1) % c->head_dim) return refuse("rows are not whole heads");
+        if (table->scalar_type() != at::kInt || table->dim() != 2 || (table->stride(1) != 1 && table->size(1) != 1) || (row_each && table->size(0) != q->size(0)))
+            return refuse("expected a block table of int32 rows, one per sequence");
+        batch = table->size(0);
+        if (!on_gpu(*table, *q) || !gpu_vector(*lengths, at::kInt, batch, *q) || !on_gpu(*ws, *q) || !same_gpu(held->device, *q) || !current(*q)) return false;
+        bytes = PyLong_AsSize_t(nbytes);
+        scale = (float)PyFloat_AsDouble(scale_);
+        if (PyErr_Occurred() || !number(window_, window)) return false;
+        if (table->size(1) > INT32_MAX || batch > INT32_MAX) return refuse("more pages than 32 bits count");
+        heads = q->size(1) / c->head_dim;
+        ld = batch == 1 ? table->size(1) : table->stride(0);
+        scores = {};
+        slopes = nullptr;
+        if (!cap) return true;
+        scores.cap = (float)PyFloat_AsDouble(cap);
+        if (PyErr_Occurred() || !maybe(slopes_, slopes) || (slopes && !gpu_vector(*slopes, at::kFloat, heads, *q))) return false;
+        scores.slopes = slopes ? (const float *)slopes->data_ptr() : nullptr;
+        return true;
+    }
+};
+
+// paged_attention(cache, Q, block_table, lengths, workspace, bytes, scale, window, O or None, with_lse[, cap, slopes or None]) -> O, or (O, lse)
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    if (n != 10) { PyErr_SetString(PyExc_TypeError, "paged_attention takes 10 arguments"); return nullptr; }
-    const CacheOn *held = structure<CacheOn>(a[0], g_cache);
-    const paro_kv_cache *c = held ? &held->c : nullptr;
-    const at::Tensor *q = c ? tensor(a[1]) : nullptr, *table = q ? tensor(a[2]) : nullptr, *lengths = table ? tensor(a[3]) : nullptr;
-    const at::Tensor *ws = lengths ? tensor(a[4]) : nullptr;
-    if (!ws || !rows(*q) || !gpu_rows(*q, -1, q->size(1), *q)) return nullptr;
-    const int64_t B = q->size(0);
-    if (c->head_dim <= 0 || q->size(1) % c->head_dim) { refuse("rows are not whole heads"); return nullptr; }
-    if (table->scalar_type() != at::kInt || table->dim() != 2 || (table->stride(1) != 1 && table->size(1) != 1) || table->size(0) != B) {
-        refuse("expected a block table of int32 rows, one per sequence");
-        return nullptr;
-    }
-    if (!on_gpu(*table, *q) || !gpu_vector(*lengths, at::kInt, B, *q) || !on_gpu(*ws, *q) || !same_gpu(held->device, *q) || !current(*q)) return nullptr;
-    const size_t bytes = PyLong_AsSize_t(a[5]);
-    const float scale = (float)PyFloat_AsDouble(a[6]);
-    int32_t window;
+    if (n != 10 && n != 12) { PyErr_SetString(PyExc_TypeError, "paged_attention takes 10 or 12 arguments"); return nullptr; }
+    Attention x;
+    if (!x.take(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], n == 12 ? a[10] : nullptr, n == 12 ? a[11] : nullptr, true)) return nullptr;
     const int want = PyObject_IsTrue(a[9]);
-    if (PyErr_Occurred() || want < 0 || !number(a[7], window)) return nullptr;
-    if (table->size(1) > INT32_MAX) { refuse("more pages than 32 bits count"); return nullptr; }
-    const int64_t heads = q->size(1) / c->head_dim, ld = B == 1 ? table->size(1) : table->stride(0);
-    at::Tensor o = rows_or_new(a[8], B, q->size(1), *q), lse;
+    if (want < 0) return nullptr;
+    at::Tensor o = rows_or_new(a[8], x.batch, x.q->size(1), *x.q), lse;
     if (!o.defined()) return nullptr;
-    if (want) lse = fresh(*q, {B, heads}, at::kFloat);
+    if (want) lse = fresh(*x.q, {x.batch, x.heads}, at::kFloat);
     void *stream = current_stream();
     paro_status st;
     Py_BEGIN_ALLOW_THREADS
-    st = paro_paged_attention(c, half_ptr(q), q->stride(0), (int32_t)heads, (const int32_t *)table->data_ptr(), ld,
-                              (int32_t)table->size(1), (const int32_t *)lengths->data_ptr(), (int32_t)B, scale, window, half_out(o),
-                              o.stride(0), want ? (float *)lse.data_ptr() : nullptr, ws->data_ptr(), bytes, stream);
+    st = paro_paged_attention_scored(x.c, half_ptr(x.q), x.q->stride(0), (int32_t)x.heads, (const int32_t *)x.table->data_ptr(), x.ld,
+                                     (int32_t)x.table->size(1), (const int32_t *)x.lengths->data_ptr(), (int32_t)x.batch, x.scale, x.window, &x.scores,
+                                     half_out(o), o.stride(0), want ? (float *)lse.data_ptr() : nullptr, x.ws->data_ptr(), x.bytes, stream);
     Py_END_ALLOW_THREADS
     if (st != PARO_OK) return PyLong_FromLong(st);
     PyObject *first = wrap(a[8], std::move(o));
     return want ? together({first, THPVariable_Wrap(std::move(lse))}) : first;
+    END_HANDLE_TH_ERRORS
+}
+
+// prompt_attention(cache, Q, starts, block_table, lengths, workspace, bytes, scale, window, cap, slopes or None, prefix or None, first or None, O or None,
+// with_lse) -> O, or (O, lse)
+PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 15) { PyErr_SetString(PyExc_TypeError, "prompt_attention takes 15 arguments"); return nullptr; }
+    Attention x;
+    if (!x.take(a[0], a[1], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], false)) return nullptr;
+    const int64_t T = x.q->size(0);
+    const at::Tensor *starts = tensor(a[2]), *prefix, *first;
+    if (!starts || !maybe(a[11], prefix) || !maybe(a[12], first)) return nullptr;
+    if (!gpu_vector(*starts, at::kInt, x.batch + 1, *x.q) || (prefix && !gpu_vector(*prefix, at::kInt, x.batch, *x.q)) ||
+        (first && !gpu_vector(*first, at::kInt, T, *x.q)))
+        return nullptr;
+    const int want = PyObject_IsTrue(a[14]);
+    if (want < 0) return nullptr;
+    at::Tensor o = rows_or_new(a[13], T, x.q->size(1), *x.q), lse;
+    if (!o.defined()) return nullptr;
+    if (want) lse = fresh(*x.q, {T, x.heads}, at::kFloat);
+    void *stream = current_stream();
+    paro_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = paro_prompt_attention(x.c, half_ptr(x.q), x.q->stride(0), (int32_t)x.heads, (int32_t)T, (const int32_t *)starts->data_ptr(),
+                               (const int32_t *)x.table->data_ptr(), x.ld, (int32_t)x.table->size(1), (const int32_t *)x.lengths->data_ptr(),
+                               (int32_t)x.batch, x.scale, x.window, &x.scores, prefix ? (const int32_t *)prefix->data_ptr() : nullptr,
+                               first ? (const int32_t *)first->data_ptr() : nullptr, half_out(o), o.stride(0),
+                               want ? (float *)lse.data_ptr() : nullptr, x.ws->data_ptr(), x.bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (st != PARO_OK) return PyLong_FromLong(st);
+    PyObject *out = wrap(a[13], std::move(o));
+    return want ? together({out, THPVariable_Wrap(std::move(lse))}) : out;
     END_HANDLE_TH_ERRORS
 }
 
@@ -377,6 +438,7 @@ PyMethodDef methods[] = {
     {"rope", (PyCFunction)(void (*)(void))rope, METH_FASTCALL, nullptr},
     {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, nullptr},
     {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
+    {"prompt_attention", (PyCFunction)(void (*)(void))prompt_attention, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "paro_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

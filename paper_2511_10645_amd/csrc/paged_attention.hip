@@ -34,7 +34,6 @@ constexpr int kQueries = 16;                     // query heads of a unit: the N
 constexpr uint32_t kLeastUnits = 4;              // of a block
 constexpr uint32_t kGroupParts = 32;             // partial results that are joined at once
 constexpr float kPShift = 15.0f;                 // p is held 2^15 times
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kRsrcRaw = 0x00020000;             // raw buffer, 32-bit data format
 constexpr int kAgent = 16;                       // agent scope: past the L2 of the XCD
 constexpr int kOnce = 2;                         // keys and values are read once: non-temporal (131071 tokens from memory: 90 us, 98 without)
@@ -66,6 +65,7 @@ struct AttnArgs {
     int page_log, n_pages, kv_heads, group, chunks, width, batch, window;
     float per_block;                             // 1 / blocks
     float scale;                                 // with log2(e)
+    Scores scores;
 };
 
 // The other three of the 4 lanes that hold one query are lanes n ^ 16, n ^ 32, n ^ 48: two exchanges of rows of lanes.
@@ -169,22 +169,29 @@ __device__ inline uint32_t f16x2_of_e4m3(uint32_t w, float scale, bool hi)
     return c.u;
 }
 
+__device__ inline uint32_t f16x2_of_e2m1(uint32_t w, float scale, int pair)
+{
+    return __builtin_bit_cast(uint32_t, pair == 0 ? f16x2_of_e2m1<0>(w, scale) : pair == 1 ? f16x2_of_e2m1<1>(w, scale) : pair == 2 ? f16x2_of_e2m1<2>(w, scale) : f16x2_of_e2m1<3>(w, scale));
+}
+
 template <int D, int FMT>
 struct Operand {
-    static constexpr int kKeyLoads = FMT == 0 ? D / 32 : D / 64;          // 16-byte requests per 16 tokens
-    static constexpr int kRowWords = D / 16 * (FMT == 0 ? 2 : 1) / 4;     // dwords of a value row in a lane
+    static constexpr int kKeyBytes = row_bytes<FMT>(D) / 4 < 16 ? row_bytes<FMT>(D) / 4 : 16;   // of a request in a lane (8: MXFP4 heads of 64 channels)
+    static constexpr int kKeyLoads = row_bytes<FMT>(D) / 4 / kKeyBytes;   // requests per 16 tokens
+    static constexpr int kRowBytes = row_bytes<FMT>(D) / 16;              // of a value row in a lane
+    static constexpr int kRowWords = (kRowBytes + 3) / 4;
 };
 
 // What a wave holds of a unit between its requests and its products.
 template <int D, int FMT>
 struct Keys {
     U4 k[2][Operand<D, FMT>::kKeyLoads];
-    uint32_t scale[2];
+    uint32_t scale[2][FMT == kMxfp4 ? Operand<D, FMT>::kKeyLoads : 1];    // E4M3: bytes of 4 tokens, MXFP4: of the request's 32 channels
 };
 template <int D, int FMT>
 struct Values {
     uint32_t v[8][Operand<D, FMT>::kRowWords];
-    uint32_t scale[2];
+    uint32_t scale[2];                           // bytes of 4 tokens
 };
 
 // One (page, head) of the cache as a buffer: a request past `bytes` returns 0 and costs nothing, which keeps the requests of a
@@ -211,10 +218,20 @@ __device__ inline void load_keys(Keys<D, FMT> &x, const AttnArgs &a, const Head 
         const __amdgpu_buffer_rsrc_t r = attn_rsrc(a.k + p * h.page_bytes + h.at, on ? h.bytes : 0);
 #pragma unroll
         for (int s = 0; s < Operand<D, FMT>::kKeyLoads; ++s)
-            x.k[i][s] = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(r, (((s * 4 + (lane >> 4)) << h.page_log) + (lane & 15)) << 4, tok << 4, kOnce));
-        if constexpr (FMT == 1) {
-            const __amdgpu_buffer_rsrc_t q = attn_rsrc(a.ks + ((p * h.kv_heads + h.head) << h.page_log), on ? 1 << h.page_log : 0);
-            x.scale[i] = __builtin_amdgcn_raw_buffer_load_b32(q, 4 * (lane >> 4), tok, kOnce);
+            if constexpr (Operand<D, FMT>::kKeyBytes == 16)
+                x.k[i][s] = __builtin_bit_cast(U4, __builtin_amdgcn_raw_buffer_load_b128(r, (((s * 4 + (lane >> 4)) << h.page_log) + (lane & 15)) << 4, tok << 4, kOnce));
+            else {
+                const U2 y = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, ((((lane >> 5) << h.page_log) + (lane & 15)) << 4) + ((lane >> 4) & 1) * 8, tok << 4, kOnce));
+                x.k[i][s] = U4{y[0], y[1], 0, 0};
+            }
+        if constexpr (FMT != kFp16) {
+            constexpr int S = row_scales<FMT>(D);
+            const __amdgpu_buffer_rsrc_t q = attn_rsrc(a.ks + (((p * h.kv_heads + h.head) * S) << h.page_log), on ? S << h.page_log : 0);
+            if constexpr (FMT == kE4m3) x.scale[i][0] = __builtin_amdgcn_raw_buffer_load_b32(q, 4 * (lane >> 4), tok, kOnce);
+            else
+#pragma unroll
+                for (int s = 0; s < Operand<D, FMT>::kKeyLoads; ++s)
+                    x.scale[i][s] = __builtin_amdgcn_raw_buffer_load_b8(q, ((D == 64 ? lane >> 5 : s * 4 + (lane >> 4)) << h.page_log) + (lane & 15), tok, kOnce);
         }
     }
 }
@@ -222,7 +239,7 @@ __device__ inline void load_keys(Keys<D, FMT> &x, const AttnArgs &a, const Head 
 template <int D, int FMT>
 __device__ inline void load_values(Values<D, FMT> &x, const AttnArgs &a, const Head &h, const int (&pg)[2], int t0, int lane)
 {
-    constexpr int W = Operand<D, FMT>::kRowWords, kRowBytes = D * (FMT == 0 ? 2 : 1);
+    constexpr int W = Operand<D, FMT>::kRowWords, kRowBytes = row_bytes<FMT>(D);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int64_t p = pg[i] < 0 ? 0 : pg[i];
@@ -230,7 +247,7 @@ __device__ inline void load_values(Values<D, FMT> &x, const AttnArgs &a, const H
         const __amdgpu_buffer_rsrc_t r = attn_rsrc(a.v + p * h.page_bytes + h.at, h.bytes);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int off = (4 * (lane >> 4) + j) * kRowBytes + (lane & 15) * (4 * W);
+            const int off = (4 * (lane >> 4) + j) * kRowBytes + (lane & 15) * Operand<D, FMT>::kRowBytes;
             uint32_t *v = x.v[4 * i + j];
             if constexpr (W % 4 == 0)
 #pragma unroll
@@ -241,18 +258,22 @@ __device__ inline void load_values(Values<D, FMT> &x, const AttnArgs &a, const H
             else if constexpr (W == 2) {
                 const U2 y = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(r, off, tok * kRowBytes, kOnce));
                 v[0] = y[0]; v[1] = y[1];
-            } else
+            } else if constexpr (Operand<D, FMT>::kRowBytes == 4)
                 v[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, tok * kRowBytes, kOnce);
+            else
+                v[0] = __builtin_amdgcn_raw_buffer_load_b16(r, off, tok * kRowBytes, kOnce);
         }
-        if constexpr (FMT == 1) {
-            const __amdgpu_buffer_rsrc_t q = attn_rsrc(a.vs + ((p * h.kv_heads + h.head) << h.page_log), 1 << h.page_log);
-            x.scale[i] = __builtin_amdgcn_raw_buffer_load_b32(q, 4 * (lane >> 4), tok, kOnce);
+        if constexpr (FMT != kFp16) {            // MXFP4: of the 32 channels that the lane's are among
+            constexpr int S = row_scales<FMT>(D);
+            const __amdgpu_buffer_rsrc_t q = attn_rsrc(a.vs + (((p * h.kv_heads + h.head) * S) << h.page_log), S << h.page_log);
+            const int group = FMT == kMxfp4 ? ((lane & 15) * (D / 16)) >> 5 : 0;
+            x.scale[i] = __builtin_amdgcn_raw_buffer_load_b32(q, (group << h.page_log) + 4 * (lane >> 4), tok, kOnce);
         }
     }
 }
 
-// log2-scaled scores of a unit: x[8], token 16 (j / 4) + 4 (lane / 16) + j % 4, query lane % 16
-template <int D, int FMT>
+// log2-scaled scores of a unit: x[8], token 16 (j / 4) + 4 (lane / 16) + j % 4, query lane % 16; RAW: without the scale
+template <int D, int FMT, bool RAW>
 __device__ inline void scores(float (&x)[8], const Keys<D, FMT> &k, const half8v (&q)[D / 32], float scale)
 {
 #pragma unroll
@@ -262,6 +283,11 @@ __device__ inline void scores(float (&x)[8], const Keys<D, FMT> &k, const half8v
         for (int s = 0; s < Operand<D, FMT>::kKeyLoads; ++s) {
             if constexpr (FMT == 0) {
                 s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, k.k[i][s]), q[s], s4, 0, 0, 0);
+            } else if constexpr (FMT == kMxfp4) {
+                const float up = __uint_as_float(k.scale[i][s] << 23);
+#pragma unroll
+                for (int w = 0; w < Operand<D, FMT>::kKeyBytes / 4; ++w)
+                    s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e2m1(k.k[i][s][w], up), q[Operand<D, FMT>::kKeyBytes / 4 * s + w], s4, 0, 0, 0);
             } else {
                 s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e4m3(k.k[i][s][0], k.k[i][s][1], 1.0f), q[2 * s], s4, 0, 0, 0);
                 s4 = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of_e4m3(k.k[i][s][2], k.k[i][s][3], 1.0f), q[2 * s + 1], s4, 0, 0, 0);
@@ -269,9 +295,24 @@ __device__ inline void scores(float (&x)[8], const Keys<D, FMT> &k, const half8v
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            x[4 * i + j] = s4[j] * scale;
-            if constexpr (FMT == 1) x[4 * i + j] *= __uint_as_float(((k.scale[i] >> (8 * j)) & 255) << 23);
+            x[4 * i + j] = RAW ? s4[j] : s4[j] * scale;
+            if constexpr (FMT == kE4m3) x[4 * i + j] *= __uint_as_float(((k.scale[i][0] >> (8 * j)) & 255) << 23);
         }
+    }
+}
+
+// Scores q . k capped, scaled to log2 and lowered by their tokens' distance from the last one, `away0` for the lane's first.
+__device__ inline void adjust(float (&x)[8], const AttnArgs &a, float slope, float away0)
+{
+    if (a.scores.cap > 0) {
+        capped(x, a.scores);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= a.scale;
+    }
+    if (a.scores.slopes) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fmaf(-slope, away0 - (16 * (j >> 2) + (j & 3)), x[j]);
     }
 }
 
@@ -286,7 +327,7 @@ __device__ inline void mask(float (&x)[8], Values<D, FMT> &v, const int (&pg)[2]
         x[j] = in ? x[j] : -INFINITY;
 #pragma unroll
         for (int w = 0; w < Operand<D, FMT>::kRowWords; ++w) v.v[j][w] = in ? v.v[j][w] : 0u;
-        if constexpr (FMT == 1) if (!in) v.scale[j >> 2] = (v.scale[j >> 2] & ~(255u << (8 * (j & 3)))) | (127u << (8 * (j & 3)));
+        if constexpr (FMT != kFp16) if (!in) v.scale[j >> 2] = (v.scale[j >> 2] & ~(255u << (8 * (j & 3)))) | (127u << (8 * (j & 3)));
     }
 }
 
@@ -332,7 +373,7 @@ __device__ inline void take_in(Running<D> &st, const float (&x)[8], const Values
         for (int r = 0; r < R; r += 2) {
             uint32_t c[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) c[j] = f16x2_of_e4m3(v.v[j][r / 4], vs[j], (r / 2) & 1);
+            for (int j = 0; j < 8; ++j) c[j] = FMT == kE4m3 ? f16x2_of_e4m3(v.v[j][r / 4 % Operand<D, FMT>::kRowWords], vs[j], (r / 2) & 1) : f16x2_of_e2m1(v.v[j][r / 8], vs[j], (r / 2) & 3);
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
                 U4 f;
@@ -508,10 +549,10 @@ __device__ inline bool arrives_last(uint32_t *counter, uint32_t all)
 // What this wave stored is where all XCDs see it.
 __device__ inline void stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-template <int D, int FMT>
+template <int D, int FMT, bool SCORED>
 __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kernel(const AttnArgs a)
 {
-    constexpr int WAVES = attn_waves<D>(), THREADS = 64 * WAVES, R = D / 16, EB = FMT == 0 ? 2 : 1;
+    constexpr int WAVES = attn_waves<D>(), THREADS = 64 * WAVES, R = D / 16;
     constexpr int kRow = D + 4;                  // floats of a row in LDS: rows of 16 queries fall on distinct banks
     extern __shared__ __attribute__((aligned(16))) float s_o[];          // [wave][2][rows][kRow], later the joins'
     __shared__ float s_m[WAVES * 2 * kQueries], s_l[WAVES * 2 * kQueries];
@@ -586,13 +627,14 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
     Head h;
     h.page_log = a.page_log;
     h.kv_heads = a.kv_heads;
-    h.bytes = (uint32_t)(D * EB) << a.page_log;
+    h.bytes = (uint32_t)row_bytes<FMT>(D) << a.page_log;
     h.page_bytes = (int64_t)h.bytes * a.kv_heads;
     Segment g;                                   // the segment at hand: units u0..u1 of it, tokens lo..hi of its sequence
     int u0, u1, lo, hi, pages = 0;
     const int32_t *row;
     Target to;
     half8v q[D / 32];
+    float slope = 0;                             // of query lane % 16
     // the pages of the next 32 units, two halves to a unit
     const auto turn = [&](int u) {
         int t = (u + (lane >> 1)) * kUnit + (lane & 1) * 16;
@@ -618,7 +660,9 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
         const _Float16 *qp = a.q + (int64_t)g.b * a.ldq + (int64_t)(to.first + (n < to.queries ? n : 0)) * D;
 #pragma unroll
         for (int s = 0; s < D / 32; ++s)
-            q[s] = *(const half8v *)(qp + (FMT == 0 ? s * 32 + quarter * 8 : ((s >> 1) * 4 + quarter) * 16 + (s & 1) * 8));
+            q[s] = *(const half8v *)(qp + (FMT == kFp16 ? s * 32 + quarter * 8 : FMT == kE4m3 ? ((s >> 1) * 4 + quarter) * 16 + (s & 1) * 8 :
+                                           D == 64 ? quarter * 16 + s * 8 : ((s >> 2) * 4 + quarter) * 32 + (s & 3) * 8));
+        if constexpr (SCORED) if (a.scores.slopes) slope = a.scores.slopes[to.first + (n < to.queries ? n : 0)] * kLog2e;
     };
     if (busy) locate(wbegin);
     __syncthreads();                             // every wave has asked for its pages before the first keys fill the way to memory
@@ -643,7 +687,8 @@ __global__ __launch_bounds__(64 * attn_waves<D>(), 1) void paged_attention_kerne
                     Values<D, FMT> v;
                     load_values<D, FMT>(v, a, h, pg, u * kUnit, lane);
                     float x[8];
-                    scores<D, FMT>(x, k, q, a.scale);
+                    scores<D, FMT, SCORED>(x, k, q, a.scale);
+                    if constexpr (SCORED) adjust(x, a, slope, (float)(hi - 1 - u * kUnit - 4 * quarter));
                     const int now[2] = {pg[0], pg[1]};
                     // the next unit's keys are on their way through this one's softmax and values
                     if (((u + 1 - u0) & 31) == 0) turn(u + 1);
@@ -788,7 +833,7 @@ static constexpr int64_t units_seen(int64_t tokens, int32_t window)
 static_assert(units_seen(4096, INT32_MAX) == 128 && units_seen(4096, 0) == 128 && units_seen(4096, 1) == 3 && units_seen(1, 1) == 1,
               "any window that an int32 holds");
 
-template <int D, int FMT>
+template <int D, int FMT, bool SCORED>
 static hipError_t launch_attention(AttnArgs &a, int64_t units, hipStream_t s)
 {
     constexpr int WAVES = attn_waves<D>();
@@ -802,14 +847,21 @@ static hipError_t launch_attention(AttnArgs &a, int64_t units, hipStream_t s)
     const size_t shares = sizeof(float) * WAVES * 2 * rows * (D + 4), joins = sizeof(float) * 6 * 64 * WAVES;
     static std::atomic<uint64_t> attr_done{0};
     if (const int dev = once_pending(attr_done); dev >= 0) {
-        const hipError_t e = hipFuncSetAttribute((const void *)paged_attention_kernel<D, FMT>, hipFuncAttributeMaxDynamicSharedMemorySize,
+        const hipError_t e = hipFuncSetAttribute((const void *)paged_attention_kernel<D, FMT, SCORED>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)(sizeof(float) * WAVES * 2 * kQueries * (D + 4)));
         if (e != hipSuccess) return e;
         once_done(attr_done, dev);
     }
-    hipLaunchKernelGGL((paged_attention_kernel<D, FMT>), dim3(blocks), dim3(64 * WAVES),
+    hipLaunchKernelGGL((paged_attention_kernel<D, FMT, SCORED>), dim3(blocks), dim3(64 * WAVES),
                        shares > joins ? shares : joins, s, a);
     return hipGetLastError();
+}
+
+template <int FMT, bool SCORED>
+static hipError_t launch_attention(int head_dim, AttnArgs &a, int64_t units, hipStream_t s)
+{
+    return head_dim == 64 ? launch_attention<64, FMT, SCORED>(a, units, s) : head_dim == 128 ? launch_attention<128, FMT, SCORED>(a, units, s) :
+                                                                                             launch_attention<256, FMT, SCORED>(a, units, s);
 }
 
 }  // namespace paro
@@ -833,13 +885,24 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
                                             const int32_t *lengths, int32_t batch, float scale, int32_t window,
                                             paro_half_t *O, int64_t ldo, float *lse, void *ws, size_t ws_bytes, void *stream)
 {
+    return paro_paged_attention_scored(cache, Q, ldq, q_heads, block_table, ld_table, table_width, lengths, batch, scale, window, nullptr, O, ldo, lse, ws,
+                                       ws_bytes, stream);
+}
+
+extern "C" paro_status paro_paged_attention_scored(const paro_kv_cache *cache, const paro_half_t *Q, int64_t ldq, int32_t q_heads,
+                                                   const int32_t *block_table, int64_t ld_table, int32_t table_width,
+                                                   const int32_t *lengths, int32_t batch, float scale, int32_t window,
+                                                   const paro_scores_t *scores, paro_half_t *O, int64_t ldo, float *lse, void *ws,
+                                                   size_t ws_bytes, void *stream)
+{
     using namespace paro;
     if (const paro_status st = check_cache(cache); st != PARO_OK) return st;
     if (!Q || !O || !block_table || !lengths) return PARO_ERR_NULL;
     const paro_kv_cache &c = *cache;
     if (batch <= 0 || q_heads <= 0 || q_heads % c.kv_heads || table_width <= 0 || window < 0) return PARO_ERR_SHAPE;
     if ((ld_table != 0 && ld_table < table_width) || O == Q) return PARO_ERR_SHAPE;
-    if (!std::isfinite(scale * kLog2e)) return PARO_ERR_SHAPE;
+    AttnArgs a;
+    if (const paro_status st = check_scores(scores, scale, a.scores); st != PARO_OK) return st;
     if (const paro_status st = check_rows(Q, ldq, (int64_t)q_heads * c.head_dim); st != PARO_OK) return st;
     if (const paro_status st = check_rows(O, ldo, (int64_t)q_heads * c.head_dim); st != PARO_OK) return st;
     if (!aligned(block_table, 4) || !aligned(lengths, 4) || (lse && !aligned(lse, 4))) return PARO_ERR_ALIGN;
@@ -852,7 +915,6 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     if (!ws || ws_bytes < paro_workspace_bytes_attention(cache, q_heads, batch)) return PARO_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return PARO_ERR_ALIGN;
 
-    AttnArgs a;
     a.k = (const uint8_t *)c.k; a.v = (const uint8_t *)c.v; a.ks = c.k_scale; a.vs = c.v_scale;
     a.q = (const _Float16 *)Q; a.table = block_table; a.lengths = lengths; a.o = (_Float16 *)O; a.lse = lse;
     a.arrived = (uint32_t *)((char *)ws + kWsPartialOff);
@@ -864,13 +926,14 @@ extern "C" paro_status paro_paged_attention(const paro_kv_cache *cache, const pa
     const int64_t most = units * units_seen(tokens, window);
     hipStream_t s = (hipStream_t)stream;
     hipError_t e;
-    switch (c.head_dim * 2 + c.format) {
-    case 128: e = launch_attention<64, 0>(a, most, s); break;
-    case 129: e = launch_attention<64, 1>(a, most, s); break;
-    case 256: e = launch_attention<128, 0>(a, most, s); break;
-    case 257: e = launch_attention<128, 1>(a, most, s); break;
-    case 512: e = launch_attention<256, 0>(a, most, s); break;
-    default: e = launch_attention<256, 1>(a, most, s); break;
+    const bool scored = a.scores.cap > 0 || a.scores.slopes;
+    switch (2 * kernel_format(c.format) + scored) {
+    case 0: e = launch_attention<kFp16, false>(c.head_dim, a, most, s); break;
+    case 1: e = launch_attention<kFp16, true>(c.head_dim, a, most, s); break;
+    case 2: e = launch_attention<kE4m3, false>(c.head_dim, a, most, s); break;
+    case 3: e = launch_attention<kE4m3, true>(c.head_dim, a, most, s); break;
+    case 4: e = launch_attention<kMxfp4, false>(c.head_dim, a, most, s); break;
+    default: e = launch_attention<kMxfp4, true>(c.head_dim, a, most, s); break;
     }
     return e == hipSuccess ? PARO_OK : PARO_ERR_HIP;
 }

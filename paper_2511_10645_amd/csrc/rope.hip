@@ -58,10 +58,36 @@ __device__ inline uint2 e4m3_codes(const float (&x)[8], float up, float most)
     return uint2{e4m3_pack(q[0], q[1], q[2], q[3]), e4m3_pack(q[4], q[5], q[6], q[7])};
 }
 
+// The exponent of 32 channels of an MXFP4 cache from their largest |value|: floor(log2 most) - 2 (6 = 1.5 * 2^2 is the largest code).
+__device__ inline int mx_exponent(float most)
+{
+    const int e = (int)(__float_as_uint(most) >> 23) - 127 - 2;
+    return e < kMxExponentLeast ? kMxExponentLeast : e > kMxExponentMost ? kMxExponentMost : e;
+}
+__device__ inline uint32_t e2m1_codes(const float (&x)[8], float scale)
+{
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+}
+// The largest |value| of 8 channels, infinite if one of them is not finite.
+__device__ inline float most_or_infinite(const float (&x)[8])
+{
+    float m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(finite_or(x[e], INFINITY)));
+    return m;
+}
+
 template <int LAYOUT, int FMT>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) float s_cs[];     // [token][cos of the pairs, sin of the pairs]
+    // MXFP4: a thread's two runs of 8 channels may belong to different groups of 32, and a group to four threads (halves are paired at
+    // any multiple of 8): the largest values of a head's runs meet here.  A head's threads are lanes of one wave, whose LDS accesses keep their order.
+    __shared__ __attribute__((aligned(16))) float s_most[FMT == kMxfp4 ? 2 * kRopeThreads : 4];
     const int t0 = blockIdx.x * a.tokens;
     const int tokens = a.T - t0 < a.tokens ? a.T - t0 : a.tokens;
     for (int i = threadIdx.x; i < tokens * a.pairs; i += kRopeThreads) {
@@ -141,7 +167,30 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a)
             continue;
         }
         const int64_t place = page0 + ((int64_t)head << a.page_log);       // this head's first token of the page
-        if constexpr (FMT == 0) {
+        if constexpr (FMT == kMxfp4) {
+            float *of_head = s_most + line * 2 * lanes;
+            of_head[ca / 8] = most_or_infinite(fa);
+            of_head[cb / 8] = most_or_infinite(fb);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            const auto of_group = [&](int channel) {
+                const float *m = of_head + channel / 32 * 4;
+                return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            };
+            const float ma = of_group(ca), mb = of_group(cb);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();         // the next head's go to the same place
+            if (!kept) continue;
+            uint8_t *y = (is_k ? a.ck : a.cv) + place * (a.D / 2), *scales = (is_k ? a.cks : a.cvs) + place * (a.D / 32);
+            const auto put = [&](const float (&f)[8], int channel, float most) {
+                const int e = mx_exponent(most);
+                const uint32_t codes = e2m1_codes(f, __uint_as_float((uint32_t)(127 + e) << 23));
+                *(uint32_t *)(y + (is_k ? ((int64_t)(channel / 32) << (a.page_log + 4)) + off * 16 + channel % 32 / 2 : (int64_t)off * (a.D / 2) + channel / 2)) = codes;
+                if (channel % 32 == 0) scales[((channel / 32) << a.page_log) + off] = (uint8_t)(most == INFINITY ? kMxNan : 127 + e);
+            };
+            put(fa, ca, ma);
+            put(fb, cb, mb);
+        } else if constexpr (FMT == 0) {
             if (!kept) continue;
             if (is_k) {
                 uint8_t *y = a.ck + place * a.D * 2 + off * 16;
@@ -189,11 +238,13 @@ static hipError_t launch_rope(RopeArgs &a, int layout, int format, hipStream_t s
     const dim3 grid((unsigned)blocks, (unsigned)((all + a.rows - 1) / a.rows));
     const size_t lds = sizeof(float) * 2 * a.tokens * (a.pairs ? a.pairs : 1);
     if (layout == 0) {
-        if (format == 0) hipLaunchKernelGGL((rope_kernel<0, 0>), grid, dim3(kRopeThreads), lds, s, a);
-        else hipLaunchKernelGGL((rope_kernel<0, 1>), grid, dim3(kRopeThreads), lds, s, a);
+        if (format == kFp16) hipLaunchKernelGGL((rope_kernel<0, kFp16>), grid, dim3(kRopeThreads), lds, s, a);
+        else if (format == kE4m3) hipLaunchKernelGGL((rope_kernel<0, kE4m3>), grid, dim3(kRopeThreads), lds, s, a);
+        else hipLaunchKernelGGL((rope_kernel<0, kMxfp4>), grid, dim3(kRopeThreads), lds, s, a);
     } else {
-        if (format == 0) hipLaunchKernelGGL((rope_kernel<1, 0>), grid, dim3(kRopeThreads), lds, s, a);
-        else hipLaunchKernelGGL((rope_kernel<1, 1>), grid, dim3(kRopeThreads), lds, s, a);
+        if (format == kFp16) hipLaunchKernelGGL((rope_kernel<1, kFp16>), grid, dim3(kRopeThreads), lds, s, a);
+        else if (format == kE4m3) hipLaunchKernelGGL((rope_kernel<1, kE4m3>), grid, dim3(kRopeThreads), lds, s, a);
+        else hipLaunchKernelGGL((rope_kernel<1, kMxfp4>), grid, dim3(kRopeThreads), lds, s, a);
     }
     return hipGetLastError();
 }
@@ -258,7 +309,7 @@ extern "C" paro_status paro_kv_append(const paro_kv_cache *cache, const paro_rop
     a.slots = slots; a.n_slots = (int64_t)c.n_pages * c.page; a.page_log = log2_of(c.page);
     a.T = T; a.D = c.head_dim;
     if (rope) { a.inv_freq = rope->inv_freq; a.positions = positions; a.magnitude = rope->magnitude; a.pairs = rope->rot_dim / 2; }
-    return launch_rope(a, rope ? rope->layout : 0, c.format, (hipStream_t)stream) == hipSuccess ? PARO_OK : PARO_ERR_HIP;
+    return launch_rope(a, rope ? rope->layout : 0, kernel_format(c.format), (hipStream_t)stream) == hipSuccess ? PARO_OK : PARO_ERR_HIP;
 }
 
 extern "C" paro_status paro_rope_frequencies_host(int32_t rot_dim, double base, int32_t scaling, double factor, double trained,
