@@ -18,6 +18,9 @@
 //
 // Few tiles with long sequences: `splits` blocks share a tile's tokens; each leaves fp32 results in the scratch, and the one that arrives
 // last joins all in their order, so that results do not depend on timing.  Nobody waits.
+#include <type_traits>
+#include <utility>
+
 #include "kv_common.h"
 
 namespace paro {
@@ -27,17 +30,27 @@ typedef float F16 __attribute__((ext_vector_type(16)));
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
 typedef uint32_t U2 __attribute__((ext_vector_type(2)));
 
-constexpr int kPairs = 32;                       // of a wave: the N of the matrix instruction
-constexpr int kWaves = 4, kTilePairs = kWaves * kPairs;
-constexpr int kTokens = 64;                      // of a tile of keys and values
-constexpr int kPromptThreads = 64 * kWaves;
+constexpr int kWaves = 4, kPromptThreads = 64 * kWaves;
 constexpr int kMaxSplits = 32;
-constexpr int kSplitBlocks = 512;                // splits make this many blocks, two for every compute unit
-constexpr int kLeastTiles = 4;                   // tiles of tokens that a split has at least
+constexpr int kSplitBlocks = 512;                // tiles are split while there are fewer of them
+constexpr int kMostParts = 2 * kSplitBlocks;     // that a call can have
+constexpr int kChip = 256;                       // compute units
+constexpr int kLeastTokens = 256;                // that a part has at least
 constexpr float kShift = 10.0f;                  // p is held 2^10 times
+constexpr float kSlack = 5.0f;                   // the maximum that p is taken from may lie so far below the true one (2^15 is an fp16 number)
 constexpr float kFarMax = 65536.0f;              // |maximum| above which scores are rounded before it is taken off
 constexpr int kPromptRaw = 0x00020000;           // raw buffer, 32-bit data format
 constexpr int kPromptAgent = 16;                 // agent scope: past the L2 of the XCD
+
+// The shape of a block: each of its waves holds 32 pairs, WN of them hold the same ones and have every WN-th run of NB x 32 tokens.
+template <int D_, int NB_, int WN_>
+struct Shape {
+    static constexpr int D = D_, NB = NB_, WN = WN_, WM = kWaves / WN_;
+    static constexpr int Pairs = 32 * WM, Tokens = 32 * NB * WN, Quarters = Tokens / 64;   // 16-token runs of a tile that a wave moves
+    static constexpr int TileBytes = Tokens * D * 2;     // of keys, and of values, as fp16 in LDS
+    static constexpr int PartFloats = Pairs * (D + 2);
+    static constexpr int Blocks = 4 * TileBytes <= 65536 ? 2 : 1;      // of a compute unit: their waves take turns at its pipes
+};
 
 struct PromptArgs {
     const uint8_t *k, *v, *ks, *vs;
@@ -46,14 +59,18 @@ struct PromptArgs {
     _Float16 *o;
     float *lse;
     uint32_t *arrived;                           // [tiles][kv_heads]
-    float *partial;                              // [tiles][kv_heads][splits] of part_floats
+    float *partial;                              // [tiles][kv_heads][splits] of PartFloats
     int64_t ldq, ldo, ld_table;
     int page_log, n_pages, kv_heads, group, width, batch, window, T, tiles, splits;
     float scale;                                 // with log2(e)
     Scores scores;
 };
 
-template <int D> constexpr size_t prompt_part_floats() { return (size_t)kTilePairs * (D + 2); }
+// f of the numbers FROM .. TO - 1, as constants.
+template <int FROM, class F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, FROM + I>()), ...); }
+template <int FROM, int TO, class F>
+__device__ __forceinline__ void each(F f) { each_of<FROM>(f, std::make_integer_sequence<int, (TO > FROM ? TO - FROM : 0)>()); }
 
 // Sums over lanes 0..lane.
 __device__ inline int prompt_sums_upto(int x)
@@ -65,6 +82,13 @@ __device__ inline int prompt_sums_upto(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);        // row_bcast 15 into rows 1 and 3
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);        // row_bcast 31 into rows 2 and 3
     return x;
+}
+// The largest of three, without the quieting of signalling NaN that fmaxf brings along (an instruction for every value).
+__device__ inline float max3(float a, float b, float c)
+{
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
 }
 // Over the lanes n and n ^ 32, which hold one pair.
 __device__ inline float max2(float x)
@@ -81,31 +105,42 @@ __device__ inline float sum2(float x)
 // A tile of pairs: of sequence b, whose rows are row0 .. row0 + rows - 1 and whose tokens are 0 .. n - 1; the tile's first pair.
 struct Where { int b, row0, rows, n, pair0; };
 
-// Tile `tile` of all sequences' tiles; false: there are fewer.  starts are taken as they come, within 0..T and not falling.
-__device__ inline bool find_tile(Where &w, const PromptArgs &a, int tile, int lane)
+// Tile `tile` of all sequences' tiles, and about how many tiles of tokens all of them have; false: there are fewer.  starts are taken as
+// they come, within 0..T and not falling.
+template <class S>
+__device__ inline bool find_tile(Where &w, int &work, const PromptArgs &a, int tile, int lane)
 {
     int before = 0;                              // tiles of the sequences seen
+    bool found = false;
+    work = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
         const int b = b0 + lane < a.batch ? b0 + lane : a.batch - 1;
-        int s0 = a.starts[b], s1 = a.starts[b + 1];
+        int s0 = a.starts[b], s1 = a.starts[b + 1], n = a.lengths[b];
+        const int room = a.width << a.page_log;
+        n = n < 0 ? 0 : n > room ? room : n;
         s0 = s0 < 0 ? 0 : s0 > a.T ? a.T : s0;
         s1 = s1 < s0 ? s0 : s1 > a.T ? a.T : s1;
-        const int tiles = b0 + lane < a.batch ? (int)(((int64_t)(s1 - s0) * a.group + kTilePairs - 1) / kTilePairs) : 0;
+        const int tiles = b0 + lane < a.batch ? (int)(((int64_t)(s1 - s0) * a.group + S::Pairs - 1) / S::Pairs) : 0;
         const int upto = prompt_sums_upto(tiles);
+        if (a.splits > 1) {
+            int seen = n - (s1 - s0) / 2;        // by a row, on average
+            if (a.window && seen > a.window) seen = a.window;
+            work += __builtin_amdgcn_readlane(prompt_sums_upto(tiles * (seen / S::Tokens + 1)), 63);
+        }
         const uint64_t behind = __ballot(before + upto > tile);
-        if (behind) {
+        if (behind && !found) {
             const int at = __builtin_ctzll(behind);
             w.b = b0 + at;
             w.row0 = __builtin_amdgcn_readlane(s0, at);
             w.rows = __builtin_amdgcn_readlane(s1, at) - w.row0;
-            w.pair0 = (tile - before - __builtin_amdgcn_readlane(upto, at) + __builtin_amdgcn_readlane(tiles, at)) * kTilePairs;
-            const int room = a.width << a.page_log, n = __builtin_amdgcn_readfirstlane(a.lengths[w.b]);
-            w.n = n < 0 ? 0 : n > room ? room : n;
-            return true;
+            w.n = __builtin_amdgcn_readlane(n, at);
+            w.pair0 = (tile - before - __builtin_amdgcn_readlane(upto, at) + __builtin_amdgcn_readlane(tiles, at)) * S::Pairs;
+            found = true;
+            if (a.splits == 1) return true;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
-    return false;
+    return found;
 }
 
 __device__ inline __amdgpu_buffer_rsrc_t prompt_rsrc(const void *p, uint32_t bytes)
@@ -113,19 +148,12 @@ __device__ inline __amdgpu_buffer_rsrc_t prompt_rsrc(const void *p, uint32_t byt
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, kPromptRaw);
 }
 
-// How a wave moves the 16 tokens of its quarter of a tile: `Loads` requests of `Bytes` a lane, `Channels` channels each.
+// How a wave moves 16 tokens of keys or of values: `Loads` requests of `Bytes` a lane, `Channels` channels each.
 template <int D, int FMT>
 struct Move {
     static constexpr int Bytes = row_bytes<FMT>(D) * 16 / 64 < 16 ? row_bytes<FMT>(D) * 16 / 64 : 16;
     static constexpr int Loads = row_bytes<FMT>(D) * 16 / 64 / Bytes;
     static constexpr int Channels = D / 4 / Loads;
-    static constexpr int Words = Bytes / 4;
-};
-template <int D, int FMT>
-struct Staged {
-    U4 k[Move<D, FMT>::Loads], v[Move<D, FMT>::Loads];
-    uint32_t ks[Move<D, FMT>::Loads], vs[Move<D, FMT>::Loads];   // scale bytes; E4M3 keys: ks[0]
-    int t0;                                      // first of the 16 tokens
 };
 template <int BYTES>
 __device__ inline U4 prompt_load(__amdgpu_buffer_rsrc_t r, int off, int base)
@@ -135,50 +163,80 @@ __device__ inline U4 prompt_load(__amdgpu_buffer_rsrc_t r, int off, int base)
     return U4{y[0], y[1], 0, 0};
 }
 
-// Asks for 16 tokens from t0 on (a multiple of 16) of page `page`; one that is not there gives zeros.
-template <int D, int FMT>
-__device__ inline void ask(Staged<D, FMT> &x, const PromptArgs &a, int head, int page, int t0, int lane)
+// 16 bytes a lane to LDS, side by side from `lds` on (the same for all lanes).
+typedef __attribute__((address_space(3))) void PromptLds;
+__device__ inline void prompt_copy(__amdgpu_buffer_rsrc_t r, uint8_t *lds, int off, int base)
 {
-    typedef Move<D, FMT> M;
-    const bool there = (uint32_t)page < (uint32_t)a.n_pages;
-    const int64_t place = ((int64_t)(there ? page : 0) * a.kv_heads + head) << a.page_log;       // the page's first token
-    const int tok = t0 & ((1 << a.page_log) - 1);
-    const uint32_t bytes = there ? (uint32_t)row_bytes<FMT>(D) << a.page_log : 0;
-    const __amdgpu_buffer_rsrc_t rk = prompt_rsrc(a.k + place * row_bytes<FMT>(D), bytes), rv = prompt_rsrc(a.v + place * row_bytes<FMT>(D), bytes);
-    x.t0 = t0;
-#pragma unroll
-    for (int i = 0; i < M::Loads; ++i) {
-        // keys: token lane % 16, run of channels lane / 16 + 4 i (8-byte runs: two to a unit)
-        const int run = (lane >> 4) + 4 * i, unit = M::Bytes == 16 ? run : run >> 1;
-        x.k[i] = prompt_load<M::Bytes>(rk, (((unit << a.page_log) + (lane & 15)) << 4) + (M::Bytes == 16 ? 0 : (run & 1) * 8), tok << 4);
-        x.v[i] = prompt_load<M::Bytes>(rv, (lane + 64 * i) * M::Bytes, tok * row_bytes<FMT>(D));
-    }
-    if constexpr (FMT != kFp16) {
-        constexpr int S = row_scales<FMT>(D);
-        const uint32_t some = there ? (uint32_t)S << a.page_log : 0;
-        const __amdgpu_buffer_rsrc_t qk = prompt_rsrc(a.ks + place * S, some), qv = prompt_rsrc(a.vs + place * S, some);
-#pragma unroll
-        for (int i = 0; i < M::Loads; ++i) {
-            const int t = (lane + 64 * i) * M::Channels / D, c = (lane + 64 * i) * M::Channels % D;
-            if (FMT == kMxfp4 || i == 0)
-                x.ks[i] = __builtin_amdgcn_raw_buffer_load_b8(qk, ((FMT == kMxfp4 ? ((lane >> 4) + 4 * i) * M::Channels / 32 : 0) << a.page_log) + (lane & 15), tok, 0);
-            x.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(qv, ((FMT == kMxfp4 ? c / 32 : 0) << a.page_log) + t, tok, 0);
-        }
-    }
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (PromptLds *)lds, 16, off, base, 0, 0);
 }
 
-// The channels of request i as fp16, 8 at a time.
-template <int D, int FMT>
-__device__ inline half8v eight(U4 x, uint32_t scale, int z)
-{
-    const float up = __uint_as_float(scale << 23);
-    if constexpr (FMT == kFp16) return __builtin_bit_cast(half8v, x);
-    if constexpr (FMT == kMxfp4) return f16_of_e2m1(x[z], up);
-    const uint32_t lo = x[2 * z], hi = x[2 * z + 1];
-    const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, up, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, up, true);
-    const half2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, up, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, up, true);
-    return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
+// LDS: keys [tokens/16][head_dim/8][16 tokens] of 16 bytes; values [tokens][head_dim] in blocks of 32 channels whose order in a row depends on
+// the row, so that the transposed reads of 4 rows at once fall on distinct banks.
+template <int D> __device__ inline int key_at(int t, int unit) { return ((t >> 4) * (D / 8) + unit) * 256 + (t & 15) * 16; }
+template <int D> __device__ inline int value_block(int t, int block) { return D == 64 ? block ^ ((t >> 1) & 1) : block ^ (t & 3); }
+template <int D> __device__ inline int value_at(int t, int c) { return t * 2 * D + value_block<D>(t, c >> 5) * 64 + (c & 31) * 2; }
+
+// 16 tokens of keys or of values on a page, from the page's memory to LDS: fp16 caches' without a way through registers, others' through x.
+template <int D, int FMT, bool KEYS>
+struct Run {
+    typedef Move<D, FMT> M;
+    static constexpr int S = row_scales<FMT>(D);
+    __amdgpu_buffer_rsrc_t r, scales;
+    int tok;
+    // of page `page`, tokens t0 (a multiple of 16) and on; a page below 0 is not there and gives zeros
+    __device__ void at(const PromptArgs &a, int head, int page, int t0)
+    {
+        const int64_t place = ((int64_t)(page < 0 ? 0 : page) * a.kv_heads + head) << a.page_log;       // the page's first token
+        tok = t0 & ((1 << a.page_log) - 1);
+        r = prompt_rsrc((KEYS ? a.k : a.v) + place * row_bytes<FMT>(D), page < 0 ? 0 : (uint32_t)row_bytes<FMT>(D) << a.page_log);
+        if constexpr (FMT != kFp16) scales = prompt_rsrc((KEYS ? a.ks : a.vs) + place * S, page < 0 ? 0 : (uint32_t)S << a.page_log);
+    }
+    // where request i of a lane lies behind the run's first byte: keys of token lane % 16, run of channels lane / 16 + 4 i (8-byte ones: two to a unit)
+    __device__ static int from(int i, int lane, int page_log)
+    {
+        if constexpr (KEYS) {
+            const int run = (lane >> 4) + 4 * i, unit = M::Bytes == 16 ? run : run >> 1;
+            return (((unit << page_log) + (lane & 15)) << 4) + (M::Bytes == 16 ? 0 : (run & 1) * 8);
+        }
+        if constexpr (FMT == kFp16) {            // the 16 bytes that come to 16 (lane + 64 i) of the run in LDS
+            const int to = (lane + 64 * i) * 16, t = to / (2 * D);
+            return t * 2 * D + value_block<D>(t, to % (2 * D) / 64) * 64 + to % 64;
+        }
+        return (lane + 64 * i) * M::Bytes;
+    }
+    __device__ int base() const { return KEYS ? tok << 4 : tok * row_bytes<FMT>(D); }
+    __device__ void copy(uint8_t *lds, int i, int lane, int page_log) const
+    {
+        prompt_copy(r, lds + i * 1024, from(i, lane, page_log), base());
+    }
+    struct Held { U4 x; uint32_t scale; };
+    __device__ void ask(Held &y, int i, int lane, int page_log) const
+    {
+        y.x = prompt_load<M::Bytes>(r, from(i, lane, page_log), base());
+        const int c = KEYS ? ((lane >> 4) + 4 * i) * M::Channels : (lane + 64 * i) * M::Channels % D, t = KEYS ? lane & 15 : (lane + 64 * i) * M::Channels / D;
+        y.scale = __builtin_amdgcn_raw_buffer_load_b8(scales, ((FMT == kMxfp4 ? c / 32 : 0) << page_log) + t, tok, 0);
+    }
+    __device__ static void put(const Held &y, uint8_t *lds, int i, int lane)
+    {
+        const float up = __uint_as_float(y.scale << 23);
+#pragma unroll
+        for (int z = 0; z < M::Channels / 8; ++z) {
+            half8v f;
+            if constexpr (FMT == kMxfp4) {
+                f = f16_of_e2m1(y.x[z], up);
+            } else {
+                const uint32_t lo = y.x[2 * (z & 1)], hi = y.x[2 * (z & 1) + 1];
+                const half2v a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, up, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, up, true);
+                const half2v c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, up, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, up, true);
+                f = half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+            }
+            const int kc = ((lane >> 4) + 4 * i) * M::Channels + 8 * z, vt = (lane + 64 * i) * M::Channels / D, vc = (lane + 64 * i) * M::Channels % D + 8 * z;
+            *(half8v *)(lds + (KEYS ? key_at<D>(lane & 15, kc / 8) : value_at<D>(vt, vc))) = f;
+        }
+    }
+};
+template <int N> __device__ __forceinline__ void prompt_wait_vm() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14)); }
+
 __device__ inline bool any_not_finite(half8v x)
 {
     const U4 u = __builtin_bit_cast(U4, x);
@@ -188,97 +246,82 @@ __device__ inline bool any_not_finite(half8v x)
     return bad;
 }
 
-// LDS: keys [head_dim/8][64 tokens] of 16 bytes; values [64 tokens][head_dim] in blocks of 32 channels whose order in a row depends on
-// the row, so that the transposed reads of 4 rows at once fall on distinct banks.
-template <int D> __device__ inline int value_block(int t, int block) { return D == 64 ? block ^ ((t >> 1) & 1) : block ^ (t & 3); }
-template <int D> __device__ inline int value_at(int t, int c) { return t * 2 * D + value_block<D>(t, c >> 5) * 64 + (c & 31) * 2; }
-template <int D> constexpr int kTileBytes = kTokens * D * 2;         // of keys, and of values
-
-// Puts the 16 tokens where the products read them.  Values of tokens past `end` are zeros (such places may hold NaN); true if `look` and a
-// value is not finite.
-template <int D, int FMT>
-__device__ inline bool put(const Staged<D, FMT> &x, uint8_t *keys, uint8_t *values, int quarter, int end, bool look, int lane)
-{
-    typedef Move<D, FMT> M;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < M::Loads; ++i) {
-        const int kc = ((lane >> 4) + 4 * i) * M::Channels, vt = (lane + 64 * i) * M::Channels / D, vc = (lane + 64 * i) * M::Channels % D;
-#pragma unroll
-        for (int z = 0; z < M::Channels / 8; ++z) {
-            *(half8v *)(keys + ((kc / 8 + z) * kTokens + quarter * 16 + (lane & 15)) * 16) = eight<D, FMT>(x.k[i], FMT == kE4m3 ? x.ks[0] : x.ks[i], z);
-            half8v y = eight<D, FMT>(x.v[i], x.vs[i], z);
-            if (look) {
-                if (x.t0 + vt >= end) y = half8v{};
-                bad |= any_not_finite(y);
-            }
-            *(half8v *)(values + value_at<D>(quarter * 16 + vt, vc + 8 * z)) = y;
-        }
-    }
-    return bad;
-}
-
 typedef __fp16 Tr4 __attribute__((__vector_size__(8)));
 typedef __attribute__((address_space(3))) Tr4 LdsTr4;
 
-template <int D, int FMT, bool SCORED>
-__global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void prompt_attention_kernel(const PromptArgs a)
+// Scores capped, scaled to log2, lowered by distance: tokens t0 + 8 (j / 4) + j % 4, `away` before the pair's position.
+__device__ inline void adjust(F16 &s, const PromptArgs &a, float slope, int away)
 {
-    constexpr int R = D / 32, KS = D / 16;       // channel tiles of the result, steps of the first product
-    extern __shared__ __attribute__((aligned(16))) uint8_t s_tiles[];        // [2] of keys and values
+    float x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = s[j];
+    if (a.scores.cap > 0) {
+        capped(x, a.scores);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] *= a.scale;
+    }
+    if (a.scores.slopes) {
+        const float from = (float)away;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = fmaf(-slope, fabsf(from - (8 * (j >> 2) + (j & 3))), x[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[j] = x[j];
+}
+
+template <class S, int FMT, bool SCORED>
+__global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_kernel(const PromptArgs a)
+{
+    constexpr int D = S::D, NB = S::NB, R = D / 32, KS = D / 16;       // channel tiles of the result, steps of the first product
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_tiles[];        // keys [2], values [2]; later the waves' results
     __shared__ int s_lo[kWaves][2], s_hi[kWaves][2];
-    __shared__ int s_bad[2];                     // 1 + the tile in this half that has values that are not finite, where not all see them
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = lane >> 5, n32 = lane & 31;
+    const int h = lane >> 5, n32 = lane & 31, wm = wave % S::WM, wn = wave / S::WM;
 
     // longest tiles first; the heads of a tile side by side, which puts a head on one XCD where there are 8 of them
     const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
     Where w;
-    if (!find_tile(w, a, tile, lane)) return;
-    const int pairs = w.rows * a.group;
+    int work;
+    if (!find_tile<S>(w, work, a, tile, lane)) return;
+    const int pairs = w.rows * a.group, pair = w.pair0 + wm * 32 + n32;
+    // the pair's row and query head (the last pair's for lanes past it)
+    const int row = (pair < pairs ? pair : pairs - 1) / a.group, qhead = head * a.group + (pair < pairs ? pair : pairs - 1) - row * a.group;
 
-    // this lane's pair and what it sees
-    const int pair = w.pair0 + wave * kPairs + n32, kept = pair < pairs ? pair : pairs - 1;
-    const int row = kept / a.group, qhead = head * a.group + kept - row * a.group;
+    // what the pair sees: lo <= t < hi, from position pos
     const int pos = w.n - w.rows + row;
     int lo = 0, hi = pos + 1;
     if (a.window) lo = pos - a.window + 1;
     if (a.first) { const int f = a.first[w.row0 + row]; lo = lo > f ? lo : f; }
     if (a.prefix) { int f = a.prefix[w.b]; f = f < w.n ? f : w.n; hi = hi > f ? hi : f; }
     lo = lo > 0 ? lo : 0;
-    const bool some = lo < hi;
-    // of the wave: the least and largest lo and hi
-    int least = some ? lo : INT32_MAX, most = some ? hi : 0;
-    int lo_most = some ? lo : INT32_MAX, hi_least = some ? hi : 0;
+    if (lo >= hi) { lo = INT32_MAX; hi = 0; }
+    int least = lo, most = hi, lo_most = lo, hi_least = hi;     // of the wave; then of the block
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         least = min(least, __shfl_xor(least, d)); most = max(most, __shfl_xor(most, d));
         lo_most = max(lo_most, __shfl_xor(lo_most, d)); hi_least = min(hi_least, __shfl_xor(hi_least, d));
     }
-    least = __builtin_amdgcn_readfirstlane(least); most = __builtin_amdgcn_readfirstlane(most);
     lo_most = __builtin_amdgcn_readfirstlane(lo_most); hi_least = __builtin_amdgcn_readfirstlane(hi_least);
     if (lane == 0) { s_lo[wave][0] = least; s_lo[wave][1] = lo_most; s_hi[wave][0] = most; s_hi[wave][1] = hi_least; }
-    if (tid < 2) s_bad[tid] = 0;
 
-    // queries: channels 16 s + 8 h .. of pair n32.  A negative scale goes into their sign, a scale of 0 makes them 0: factors of maxima are positive.
+    // its query: channels 16 s + 8 h ..  A negative scale goes into the queries' sign, a scale of 0 makes them 0: factors of maxima are positive.
     half8v q[KS];
     {
         const _Float16 *qp = a.q + (int64_t)(w.row0 + row) * a.ldq + (int64_t)qhead * D + 8 * h;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            q[s] = *(const half8v *)(qp + 16 * s);
-            if constexpr (!SCORED) {
-                if (a.scale < 0) q[s] = -q[s];
-                if (a.scale == 0) q[s] *= (_Float16)0;
-            }
-        }
+        for (int s = 0; s < KS; ++s) q[s] = *(const half8v *)(qp + 16 * s);
+        if constexpr (!SCORED)
+            if (a.scale <= 0)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) q[s] = a.scale < 0 ? -q[s] : q[s] * (_Float16)0;
     }
     const float scale = SCORED ? 1.0f : a.scale == 0 ? 1.0f : fabsf(a.scale);
     float slope = 0;
     if constexpr (SCORED) if (a.scores.slopes) slope = a.scores.slopes[qhead] * kLog2e;
     __syncthreads();
-    int begin = s_lo[0][0], end = s_hi[0][0], whole_lo = s_lo[0][1], whole_hi = s_hi[0][1];      // of the block
+    int begin = s_lo[0][0], end = s_hi[0][0], whole_lo = s_lo[0][1], whole_hi = s_hi[0][1];
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) {
         begin = min(begin, s_lo[i][0]); end = max(end, s_hi[i][0]);
@@ -286,10 +329,16 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void prompt_atten
     }
     begin = __builtin_amdgcn_readfirstlane(begin); end = __builtin_amdgcn_readfirstlane(end);
     whole_lo = __builtin_amdgcn_readfirstlane(whole_lo); whole_hi = __builtin_amdgcn_readfirstlane(whole_hi);
-    // tiles of tokens, and this split's share of them
-    const int tile0 = begin < end ? begin / kTokens : 0, tiles = begin < end ? (end + kTokens - 1) / kTokens - tile0 : 0;
-    int parts = tiles / kLeastTiles;
-    parts = parts < 1 ? 1 : parts > a.splits ? a.splits : parts;
+    // tiles of tokens, and this split's share of them: parts are as long as a block's share of all work
+    const int tile0 = begin < end ? begin / S::Tokens : 0, tiles = begin < end ? (end + S::Tokens - 1) / S::Tokens - tile0 : 0;
+    int parts = 1;
+    if (a.splits > 1) {
+        constexpr int Least = kLeastTokens / S::Tokens;
+        const int64_t mean = ((int64_t)work * a.kv_heads + kChip * S::Blocks - 1) / (kChip * S::Blocks);
+        const int part = mean < Least ? Least : mean < tiles ? (int)mean : tiles;
+        parts = min(a.splits, part ? (tiles + part - 1) / part : 1);
+        if (parts < 1) parts = 1;
+    }
     if (split >= parts) return;
     const int per = (tiles + parts - 1) / parts;
     const int u0 = tile0 + split * per, u1 = min(u0 + per, tile0 + tiles);       // u0 may lie past u1: an empty share
@@ -299,184 +348,353 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void prompt_atten
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[r][j] = 0;
-    float m = -INFINITY, l = 0;                  // of the pair; l over this lane's tokens only
+    float m = -INFINITY, l = 0, up = scale, off = kShift;       // p = 2^(up s + off) of a score s is taken from the maximum m; l over this lane's tokens only
 
+    // The pages of 64 runs of 16 tokens from run0 on, one to a lane (-1: not there, or past the part's tokens), and which of them are there.
     const int32_t *table = a.table + (int64_t)w.b * a.ld_table;
-    // the page of this wave's quarter of tile u; -1 past the end
-    const auto page_of = [&](int u) {
-        const int t = u * kTokens + wave * 16;
-        return t < end && u < u1 ? __builtin_amdgcn_readfirstlane(table[t >> a.page_log]) : -1;
+    constexpr int Runs = S::Tokens / 16;         // of a tile
+    int run0 = u0 * Runs, pages = -1;
+    uint64_t there = 0;
+    const auto turn = [&](int run) {
+        run0 = run;
+        const int t = (run + lane) * 16;
+        pages = -1;
+        if (t < end && run + lane < u1 * Runs) {
+            const int p = table[t >> a.page_log];
+            pages = (uint32_t)p < (uint32_t)a.n_pages ? p : -1;
+        }
+        there = __ballot(pages >= 0);
     };
-    // a tile that some pair does not see all of, or that has a page missing, which its quarter alone knows
-    const auto at_edge = [&](int u) { return u * kTokens < whole_lo || (u + 1) * kTokens > whole_hi; };
-    __shared__ int s_gone[2][kWaves];            // 1: the quarter's page is not there
-    Staged<D, FMT> x;
-    const auto fill = [&](int u, int page) {
-        uint8_t *to = s_tiles + (u & 1) * 2 * kTileBytes<D>;
-        const bool bad = put<D, FMT>(x, to, to + kTileBytes<D>, wave, end, at_edge(u), lane);
-        if (at_edge(u) && __ballot(bad) && lane == 0) s_bad[u & 1] = u + 1;
-        if (lane == 0) s_gone[u & 1][wave] = (uint32_t)page >= (uint32_t)a.n_pages;
+    struct Pages { int page[S::Quarters]; uint32_t gone; };      // of this wave's runs of a tile; a bit for every run of the tile that is not there
+    const auto pages_of = [&](int u) {
+        if (u * Runs - run0 >= 64) turn(u * Runs);
+        Pages p;
+#pragma unroll
+        for (int i = 0; i < S::Quarters; ++i) p.page[i] = __builtin_amdgcn_readlane(pages, u * Runs - run0 + wave + 4 * i);
+        p.gone = (uint32_t)(~(there >> (u * Runs - run0))) & ((1u << Runs) - 1);
+        return p;
     };
-    int page = page_of(u0), next_page = page_of(u0 + 1);
+    const auto keys_of = [&](int u) { return s_tiles + (u & 1) * S::TileBytes; };
+    const auto values_of = [&](int u) { return s_tiles + (2 + (u & 1)) * S::TileBytes; };
+    constexpr int Loads = Move<D, FMT>::Loads, Jobs = S::Quarters * Loads;       // requests of a wave for its share of a tile's keys, and of its values
+    constexpr bool Copied = FMT == kFp16;
+    Run<D, FMT, true> kr[S::Quarters];
+    Run<D, FMT, false> vr[S::Quarters];
+    typename Run<D, FMT, true>::Held kh[Copied ? 1 : Jobs];
+    typename Run<D, FMT, false>::Held vh[Copied ? 1 : Jobs];
+    const auto keys_at = [&](const Pages &p, int u) {
+#pragma unroll
+        for (int i = 0; i < S::Quarters; ++i) kr[i].at(a, head, p.page[i], u * S::Tokens + (wave + 4 * i) * 16);
+    };
+    const auto values_at = [&](const Pages &p, int u) {
+#pragma unroll
+        for (int i = 0; i < S::Quarters; ++i) vr[i].at(a, head, p.page[i], u * S::Tokens + (wave + 4 * i) * 16);
+    };
+    const auto key_run = [&](int u, int job) { return keys_of(u) + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
+    const auto value_run = [&](int u, int job) { return values_of(u) + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
+
+    // S^T of a tile: score j of block b is of token 32 (NB wn + b) + 8 (j / 4) + 4 h + j % 4
+    F16 s[NB];
+    const int key_lane = key_at<D>(32 * NB * wn + n32, h);
+    const auto key_frag = [&](const uint8_t *keys, int i) { return *(const half8v *)(keys + key_lane + key_at<D>(32 * (i / KS), 2 * (i % KS))); };
+    // 16 tokens i / R of this wave's, channels 32 (i % R) .., transposed; tokens 4 h + (0..3), then 8 more
+    int value_lane[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) value_lane[r] = value_at<D>(32 * NB * wn + 4 * h + ((lane & 15) >> 2), 32 * r + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+    const auto value_frag = [&](const uint8_t *values, int i) {
+        const uint8_t *from = values + value_lane[i % R] + 16 * (i / R) * 2 * D;
+        const Tr4 one = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsTr4 *)from), two = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsTr4 *)(from + 8 * 2 * D));
+        half8v f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { f[e] = (_Float16)one[e]; f[4 + e] = (_Float16)two[e]; }
+        return f;
+    };
+    // what is done to scores before their maximum is taken: other scores, and the mask
+    const auto finish = [&](F16 (&z)[NB], int u, uint32_t gone) {
+        const int t0 = u * S::Tokens + 32 * NB * wn + 4 * h;
+        if constexpr (SCORED) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) adjust(z[b], a, slope, pos - t0 - 32 * b);
+        }
+        if (u * S::Tokens < lo_most || (u + 1) * S::Tokens > hi_least || gone) {
+            const int from = lo - t0, to = hi - t0;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int t = 32 * b + 8 * (j >> 2) + (j & 3);
+                    const bool in = t >= from && t < to && !((gone >> (2 * (NB * wn + b) + (j >> 3))) & 1);
+                    z[b][j] = in ? z[b][j] : -INFINITY;
+                }
+        }
+    };
+    // new scores z, the largest of this lane's `top`: the sums follow if the maximum has grown by more than kSlack
+    const auto follow = [&](float top, F16 (&z)[NB]) {
+        top = max2(top) * scale;
+        if (__ballot(top > m + kSlack)) {
+            const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+            m = fmaxf(m, top);
+            l *= f;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[r][j] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        up = scale;
+        off = kShift - ref;
+        if (__ballot(fabsf(ref) > kFarMax)) {
+            // product and difference as one would be off by up to half a unit of the maximum here, and p has to stay within fp16
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float y = z[b][j] * scale;
+                    z[b][j] = y - ref;
+                }
+            up = 1.0f;
+            off = kShift;
+        }
+    };
+
     if (u0 < u1) {
-        ask<D, FMT>(x, a, head, page, u0 * kTokens + wave * 16, lane);
-        fill(u0, page);
-        page = next_page;
-        ask<D, FMT>(x, a, head, page, (u0 + 1) * kTokens + wave * 16, lane);
-        next_page = page_of(u0 + 2);
-    }
-    __syncthreads();
-    for (int u = u0; u < u1; ++u) {
-        if (u + 1 < u1) {
-            fill(u + 1, page);
-            page = next_page;
-            ask<D, FMT>(x, a, head, page, (u + 2) * kTokens + wave * 16, lane);
-            next_page = page_of(u + 3);
-        }
-        uint8_t *keys = s_tiles + (u & 1) * 2 * kTileBytes<D>, *values = keys + kTileBytes<D>;
-        const int t0 = u * kTokens;
-        int gone = 0;
+        turn(run0);
+        Pages p1 = pages_of(u0 + 1), p2 = pages_of(u0 + 2);
+        {
+            const Pages p0 = pages_of(u0);
+            keys_at(p0, u0);
+            values_at(p0, u0);
+            if constexpr (Copied) {
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) gone |= s_gone[u & 1][i] << i;
-        gone = __builtin_amdgcn_readfirstlane(gone);
-        if (__builtin_amdgcn_readfirstlane(s_bad[u & 1]) == u + 1) {
-            // Values that are not finite, where some pair does not see them: a weight of 0 would not keep them out of the product.  Those that do see
-            // them take them here (their results are not finite, whatever the weight is); then zeros take their place.
-            for (int t = t0; t < t0 + kTokens && t < end; ++t) {
-                const bool seen = t >= lo && t < hi;
+                for (int i = 0; i < Jobs; ++i) kr[i / Loads].copy(key_run(u0, i), i % Loads, lane, a.page_log);
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+                for (int i = 0; i < Jobs; ++i) vr[i / Loads].copy(value_run(u0, i), i % Loads, lane, a.page_log);
+                keys_at(p1, u0 + 1);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float y = (float)*(const _Float16 *)(values + value_at<D>(t - t0, 32 * r + 8 * (j >> 2) + 4 * h + (j & 3)));
-                        if (seen && !is_finite(y)) acc[r][j] += y;
-                    }
-            }
-            __syncthreads();
-            for (int i = tid; i < kTileBytes<D> / 16; i += kPromptThreads) {
-                half8v y = *(half8v *)(values + 16 * i);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = is_finite((float)y[e]) ? y[e] : (_Float16)0;
-                *(half8v *)(values + 16 * i) = y;
-            }
-            __syncthreads();
-        }
-        if (t0 < most && t0 + kTokens > least) {
-            float s[2][16];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                F16 z;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) z[j] = 0;
-#pragma unroll
-                for (int i = 0; i < KS; ++i)
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8v *)(keys + ((2 * i + h) * kTokens + 32 * b + n32) * 16), q[i], z, 0, 0, 0);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[b][j] = z[j];
-            }
-            if constexpr (SCORED) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    if (a.scores.cap > 0) {
-                        capped(s[b], a.scores);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) s[b][j] *= a.scale;
-                    }
-                    if (a.scores.slopes) {
-                        const float away = (float)(pos - t0 - 4 * h - 32 * b);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) s[b][j] = fmaf(-slope, fabsf(away - (8 * (j >> 2) + (j & 3))), s[b][j]);
-                    }
-                }
-            }
-            // token 32 b + 8 (j / 4) + 4 h + j % 4 of the tile
-            if (t0 < lo_most || t0 + kTokens > hi_least || gone) {
-                const int from = lo - t0 - 4 * h, to = hi - t0 - 4 * h;
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const int t = 32 * b + 8 * (j >> 2) + (j & 3);
-                        const bool in = t >= from && t < to && !((gone >> (2 * b + (j >> 3))) & 1);
-                        s[b][j] = in ? s[b][j] : -INFINITY;
-                    }
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
-            top = fmaxf(m, max2(top) * scale);
-            if (__ballot(top > m)) {
-                const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
-                l *= f;
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[r][j] *= f;
-                m = top;
-            }
-            const float ref = m == -INFINITY ? 0.0f : m;
-            if (__ballot(fabsf(ref) > kFarMax)) {
-                // product and difference as one would be off by up to half a unit of the maximum here, and p has to stay within fp16
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float y = s[b][j] * scale;
-                        s[b][j] = __builtin_amdgcn_exp2f((y - ref) + kShift);
-                        l += s[b][j];
-                    }
+                for (int i = 0; i < Jobs; ++i) kr[i / Loads].copy(key_run(u0 + 1, i), i % Loads, lane, a.page_log);
+                prompt_wait_vm<0>();
             } else {
-                const float off = kShift - ref;
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int i = 0; i < Jobs; ++i) kr[i / Loads].ask(kh[i], i % Loads, lane, a.page_log);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        s[b][j] = __builtin_amdgcn_exp2f(fmaf(s[b][j], scale, off));
-                        l += s[b][j];
-                    }
-            }
-            // O^T += V^T P^T, 16 tokens a step
-            const int l16 = lane & 15;
+                for (int i = 0; i < Jobs; ++i) vr[i / Loads].ask(vh[i], i % Loads, lane, a.page_log);
+                keys_at(p1, u0 + 1);
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                half8v p;
+                for (int i = 0; i < Jobs; ++i) {
+                    kr[0].put(kh[i], key_run(u0, i), i % Loads, lane);
+                    kr[i / Loads].ask(kh[i], i % Loads, lane, a.page_log);
+                }
+                values_at(p1, u0 + 1);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (_Float16)s[st >> 1][8 * (st & 1) + e];
+                for (int i = 0; i < Jobs; ++i) {
+                    vr[0].put(vh[i], value_run(u0, i), i % Loads, lane);
+                    vr[i / Loads].ask(vh[i], i % Loads, lane, a.page_log);
+                }
+                keys_at(p2, u0 + 2);
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int t = 16 * st + 4 * h + (l16 >> 2), c = 32 * r + 16 * ((lane >> 4) & 1) + 4 * (l16 & 3);
-                    const Tr4 one = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsTr4 *)(values + value_at<D>(t, c)));
-                    const Tr4 two = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsTr4 *)(values + value_at<D>(t + 8, c)));
-                    half8v f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { f[e] = (_Float16)one[e]; f[4 + e] = (_Float16)two[e]; }
-                    acc[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, p, acc[r], 0, 0, 0);
+                for (int i = 0; i < Jobs; ++i) {
+                    kr[0].put(kh[i], key_run(u0 + 1, i), i % Loads, lane);
+                    kr[i / Loads].ask(kh[i], i % Loads, lane, a.page_log);
                 }
             }
+            __syncthreads();
+            const uint8_t *keys = keys_of(u0);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[b][j] = 0;
+#pragma unroll
+            for (int i = 0; i < NB * KS; ++i) s[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_frag(keys, i), q[i % KS], s[i / KS], 0, 0, 0);
+            finish(s, u0, p0.gone);
+            float top = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) top = max3(top, s[b][j], s[b][j + 1]);
+            follow(top, s);
         }
-        __syncthreads();
+        // A round has the scores of tile u.  It turns them into weights while the matrix cores compute those of u + 1, then multiplies the weights
+        // with the values of u while it looks for the next maximum; keys of u + 2 and values of u + 1 go to LDS meanwhile.  What the vector units do is dealt
+        // out over the matrix instructions evenly, 32 cycles of a matrix core to as many of a vector unit: 8 each for the issue and for an exponential, 4 for others.
+        for (int u = u0; u < u1; ++u) {
+            uint8_t *values = values_of(u);
+            if (u * S::Tokens < whole_lo || (u + 1) * S::Tokens > whole_hi) {
+                // A tile that some pair does not see all of: values that nobody sees become zeros, for such places may hold NaN, whose product with a weight
+                // of 0 is not 0.  Others that are not finite are taken here by the pairs that see them (their results are not finite, whatever the
+                // weight is) before zeros take their place.
+                bool bad = false;
+#pragma unroll
+                for (int k = 0; k < S::TileBytes / 16 / kPromptThreads; ++k) {
+                    const int i = tid + k * kPromptThreads;
+                    half8v *y = (half8v *)(values + 16 * i);
+                    if (u * S::Tokens + i / (D / 8) >= end) *y = half8v{};
+                    else bad |= any_not_finite(*y);
+                }
+                if (__syncthreads_or(bad)) {
+                    for (int i = 32 * NB * wn; i < 32 * NB * (wn + 1); ++i) {
+                        const bool seen = u * S::Tokens + i >= lo && u * S::Tokens + i < hi;
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const float y = (float)*(const _Float16 *)(values + value_at<D>(i, 32 * r + 8 * (j >> 2) + 4 * h + (j & 3)));
+                                if (seen && !is_finite(y)) acc[r][j] += y;
+                            }
+                    }
+                    __syncthreads();
+                    for (int i = tid; i < S::TileBytes / 16; i += kPromptThreads) {
+                        half8v y = *(half8v *)(values + 16 * i);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = is_finite((float)y[e]) ? y[e] : (_Float16)0;
+                        *(half8v *)(values + 16 * i) = y;
+                    }
+                    __syncthreads();
+                }
+            }
+            const uint32_t gone = p1.gone;
+            if constexpr (Copied) {              // keys of u + 2, values of u + 1; past the part's last tile there is nothing to read, and zeros come
+                values_at(p1, u + 1);
+                keys_at(p2, u + 2);
+                p1 = p2;
+                p2 = pages_of(u + 3);
+            } else {                             // those are held, and are put down before the next are asked for
+                values_at(p2, u + 2);
+                p1 = p2;
+                p2 = pages_of(u + 3);
+                keys_at(p2, u + 3);
+            }
+
+            constexpr int All = NB * 8, Late = NB * 3;       // pairs of scores; those whose weights the second product does not need at once
+            half8v p[2 * NB];
+            const auto weigh = [&](auto at) {
+                constexpr int c = at, b = c / 8, e = c % 8;
+                const float one = __builtin_amdgcn_exp2f(fmaf(s[b][2 * e], up, off)), two = __builtin_amdgcn_exp2f(fmaf(s[b][2 * e + 1], up, off));
+                l += one;
+                l += two;
+                half2v both = {(_Float16)one, (_Float16)two};
+                asm volatile("" : "+v"(both), "+v"(l));      // here, not where they are needed
+                p[c / 4][2 * (e & 3)] = both[0];
+                p[c / 4][2 * (e & 3) + 1] = both[1];
+            };
+            F16 next[NB];
+            {
+                constexpr int Steps = NB * KS;
+                const uint8_t *keys = keys_of(u + 1);
+                half8v f[3] = {key_frag(keys, 0), key_frag(keys, 1)};
+                each<0, Steps>([&](auto at) {
+                    constexpr int i = at;
+                    if constexpr (i + 2 < Steps) f[(i + 2) % 3] = key_frag(keys, i + 2);
+                    F16 z = next[i / KS];
+                    if constexpr (i % KS == 0)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) z[j] = 0;
+                    next[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % 3], q[i % KS], z, 0, 0, 0);
+                    if constexpr (Copied)
+                        each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) {
+                            constexpr int k = job;
+                            if constexpr (k < Jobs) kr[k / Loads].copy(key_run(u + 2, k), k % Loads, lane, a.page_log);
+                            else vr[(k - Jobs) / Loads].copy(value_run(u + 1, k - Jobs), (k - Jobs) % Loads, lane, a.page_log);
+                        });
+                    each<i *(All - Late) / Steps, (i + 1) * (All - Late) / Steps>(weigh);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            }
+            finish(next, u + 1, gone);
+            float top = -INFINITY;
+            {
+                constexpr int Steps = 2 * NB * R, Soon = NB * R;
+                half8v f[3] = {value_frag(values, 0), value_frag(values, 1)};
+                each<0, Steps>([&](auto at) {
+                    constexpr int i = at;
+                    if constexpr (i + 2 < Steps) f[(i + 2) % 3] = value_frag(values, i + 2);
+                    acc[i % R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % 3], p[i / R], acc[i % R], 0, 0, 0);
+                    if constexpr (i < Soon) each<All - Late + i * Late / Soon, All - Late + (i + 1) * Late / Soon>(weigh);
+                    each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) {
+                        constexpr int c = two;
+                        top = max3(top, next[c / 8][2 * (c % 8)], next[c / 8][2 * (c % 8) + 1]);
+                    });
+                    if constexpr (!Copied)
+                        each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) {
+                            constexpr int k = job;
+                            if constexpr (k < Jobs) {
+                                kr[0].put(kh[k], key_run(u + 2, k), k % Loads, lane);
+                                kr[k / Loads].ask(kh[k], k % Loads, lane, a.page_log);
+                            } else {
+                                vr[0].put(vh[k - Jobs], value_run(u + 1, k - Jobs), (k - Jobs) % Loads, lane);
+                                vr[(k - Jobs) / Loads].ask(vh[k - Jobs], (k - Jobs) % Loads, lane, a.page_log);
+                            }
+                        });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s[b] = next[b];
+            follow(top, s);
+            if constexpr (Copied) prompt_wait_vm<0>();
+            __syncthreads();
+        }
     }
     l = sum2(l);
 
+    if constexpr (S::WN > 1) {
+        // the waves that share pairs: their results meet in LDS, and each finishes every WN-th run of 4 registers
+        float *sums = (float *)s_tiles;          // [wave][R][4][64] of 4
+        __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(F4 *)(sums + (((wave * R + r) * 4 + i) * 64 + lane) * 4) = F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]};
+        if (h == 0) { s_m[wave][n32] = m; s_l[wave][n32] = l; }
+        __syncthreads();
+        float f[S::WN];
+        m = -INFINITY;
+#pragma unroll
+        for (int z = 0; z < S::WN; ++z) m = fmaxf(m, s_m[wm + z * S::WM][n32]);
+        const float ref = m == -INFINITY ? 0.0f : m;
+        l = 0;
+#pragma unroll
+        for (int z = 0; z < S::WN; ++z) {
+            f[z] = __builtin_amdgcn_exp2f(s_m[wm + z * S::WM][n32] - ref);
+            l = fmaf(s_l[wm + z * S::WM][n32], f[z], l);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i % S::WN != wn) continue;
+                F4 y = {0, 0, 0, 0};
+#pragma unroll
+                for (int z = 0; z < S::WN; ++z) {
+                    const F4 v = *(const F4 *)(sums + ((((wm + z * S::WM) * R + r) * 4 + i) * 64 + lane) * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = fmaf(v[e], f[z], y[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[r][4 * i + e] = y[e];
+            }
+    }
+    const auto mine = [&](int i) { return S::WN == 1 || i % S::WN == wn; };      // runs of 4 registers that this wave finishes
+
     if (parts > 1) {
         // every part's m, l and sums where its lanes left them, through memory that all XCDs see
-        const size_t tile_at = (size_t)(tile * a.kv_heads + head);
-        const auto part_rsrc = [&](int p) { return prompt_rsrc(a.partial + (tile_at * a.splits + p) * prompt_part_floats<D>(), (uint32_t)(prompt_part_floats<D>() * 4)); };
-        const int ml_at = (kTilePairs * D + 2 * (wave * kPairs + n32)) * 4;
-        const auto sums_at = [&](int r, int i) { return (((wave * R + r) * 4 + i) * 64 + lane) * 16; };
+        const size_t tile_at = (size_t)tile * a.kv_heads + head;
+        const auto part_rsrc = [&](int p) { return prompt_rsrc(a.partial + (tile_at * a.splits + p) * S::PartFloats, (uint32_t)(S::PartFloats * 4)); };
+        const int ml_at = (S::Pairs * D + 2 * (wm * 32 + n32)) * 4;
+        const auto sums_at = [&](int r, int i) { return (((wm * R + r) * 4 + i) * 64 + lane) * 16; };
         typedef decltype(__builtin_amdgcn_raw_buffer_load_b128(part_rsrc(0), 0, 0, 0)) B4;
         typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(part_rsrc(0), 0, 0, 0)) B2;
         {
             const __amdgpu_buffer_rsrc_t to = part_rsrc(split);
-            if (h == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B2, U2{__float_as_uint(m), __float_as_uint(l)}), to, ml_at, 0, kPromptAgent);
+            if (h == 0 && wn == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B2, U2{__float_as_uint(m), __float_as_uint(l)}), to, ml_at, 0, kPromptAgent);
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]}), to, sums_at(r, i), 0, kPromptAgent);
+                    if (mine(i))
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]}), to, sums_at(r, i), 0,
+                                                               kPromptAgent);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -488,10 +706,9 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void prompt_atten
         }
         __syncthreads();
         if (!__builtin_amdgcn_readfirstlane(s_last)) return;
-        float top = -INFINITY;
-        for (int p = 0; p < parts; ++p) top = fmaxf(top, __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part_rsrc(p), ml_at, 0, kPromptAgent)));
-        const float ref = top == -INFINITY ? 0.0f : top;
-        m = top;
+        m = -INFINITY;
+        for (int p = 0; p < parts; ++p) m = fmaxf(m, __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part_rsrc(p), ml_at, 0, kPromptAgent)));
+        const float ref = m == -INFINITY ? 0.0f : m;
         l = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -504,13 +721,15 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void prompt_atten
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[r][i] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(from, sums_at(r, i), 0, kPromptAgent));
+                for (int i = 0; i < 4; ++i)
+                    if (mine(i)) y[r][i] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(from, sums_at(r, i), 0, kPromptAgent));
             const float f = __builtin_amdgcn_exp2f(__uint_as_float(ml[0]) - ref);
             l = fmaf(__uint_as_float(ml[1]), f, l);
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[r][j] = fmaf(y[r][j >> 2][j & 3], f, acc[r][j]);
+                for (int j = 0; j < 16; ++j)
+                    if (mine(j >> 2)) acc[r][j] = fmaf(y[r][j >> 2][j & 3], f, acc[r][j]);
         }
     }
 
@@ -521,51 +740,70 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void prompt_atten
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(half4v *)(o + 32 * r + 8 * i) = half4v{(_Float16)(acc[r][4 * i] * inv), (_Float16)(acc[r][4 * i + 1] * inv), (_Float16)(acc[r][4 * i + 2] * inv),
-                                                       (_Float16)(acc[r][4 * i + 3] * inv)};
-        if (a.lse && h == 0)
+                if (mine(i))
+                    *(half4v *)(o + 32 * r + 8 * i) = half4v{(_Float16)(acc[r][4 * i] * inv), (_Float16)(acc[r][4 * i + 1] * inv), (_Float16)(acc[r][4 * i + 2] * inv),
+                                                           (_Float16)(acc[r][4 * i + 3] * inv)};
+        if (a.lse && h == 0 && wn == 0)
             a.lse[(int64_t)(w.row0 + row) * (a.kv_heads * a.group) + qhead] = l == 0.0f ? -INFINITY : (m - kShift + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
 
-// Tiles that T rows of `batch` sequences can have at most.
-static int64_t prompt_tiles(int64_t T, int64_t group, int64_t batch)
+// Most tiles of `pairs` pairs that T rows of `batch` sequences can have.
+static int64_t prompt_tiles(int64_t T, int64_t group, int64_t batch, int pairs)
 {
     const int64_t all = T * group;
-    return batch == 1 ? (all + kTilePairs - 1) / kTilePairs : all / kTilePairs + (batch < T ? batch : T);
+    return batch == 1 ? (all + pairs - 1) / pairs : all / pairs + (batch < T ? batch : T);
 }
-// Blocks that share a tile: as many as make kSplitBlocks blocks.
+// Most parts that a tile is cut into.
 static int64_t prompt_splits(int64_t tiles, int64_t kv_heads)
 {
     const int64_t heads = tiles * kv_heads, n = (kSplitBlocks + heads - 1) / heads;
     return n < kMaxSplits ? n : kMaxSplits;
 }
 
-template <int D, int FMT, bool SCORED>
-static hipError_t launch_prompt(const PromptArgs &a, hipStream_t s)
+// The shapes that calls choose from, by what they have of pairs.
+template <int D> struct Shapes;
+template <> struct Shapes<64> { typedef Shape<64, 2, 1> Many; typedef Shape<64, 1, 4> Few; };
+template <> struct Shapes<128> { typedef Shape<128, 2, 1> Many; typedef Shape<128, 1, 4> Few; };
+template <> struct Shapes<256> { typedef Shape<256, 2, 1> Many; typedef Shape<256, 1, 2> Few; };
+constexpr int kFewPairs = 64;                    // of a sequence on average, up to which
+
+template <class S, int FMT, bool SCORED>
+static hipError_t launch_prompt(PromptArgs &a, hipStream_t s)
 {
-    constexpr int lds = 4 * kTileBytes<D>;
+    constexpr int lds = 4 * S::TileBytes;
     static std::atomic<uint64_t> attr_done{0};
     if (const int dev = once_pending(attr_done); dev >= 0) {
-        const hipError_t e = hipFuncSetAttribute((const void *)prompt_attention_kernel<D, FMT, SCORED>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        const hipError_t e = hipFuncSetAttribute((const void *)prompt_attention_kernel<S, FMT, SCORED>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
         once_done(attr_done, dev);
     }
-    hipLaunchKernelGGL((prompt_attention_kernel<D, FMT, SCORED>), dim3((unsigned)(a.tiles * a.kv_heads * a.splits)), dim3(kPromptThreads), lds, s, a);
+    a.tiles = (int)prompt_tiles(a.T, a.group, a.batch, S::Pairs);
+    a.splits = (int)prompt_splits(a.tiles, a.kv_heads);
+    hipLaunchKernelGGL((prompt_attention_kernel<S, FMT, SCORED>), dim3((unsigned)(a.tiles * a.kv_heads * a.splits)), dim3(kPromptThreads), lds, s, a);
     return hipGetLastError();
 }
+template <int D, int FMT, bool SCORED>
+static hipError_t launch_prompt(PromptArgs &a, hipStream_t s)
+{
+    if ((int64_t)a.T * a.group <= (int64_t)kFewPairs * a.batch) return launch_prompt<typename Shapes<D>::Few, FMT, SCORED>(a, s);
+    return launch_prompt<typename Shapes<D>::Many, FMT, SCORED>(a, s);
+}
 template <int FMT, bool SCORED>
-static hipError_t launch_prompt(int head_dim, const PromptArgs &a, hipStream_t s)
+static hipError_t launch_prompt(int head_dim, PromptArgs &a, hipStream_t s)
 {
     return head_dim == 64 ? launch_prompt<64, FMT, SCORED>(a, s) : head_dim == 128 ? launch_prompt<128, FMT, SCORED>(a, s) : launch_prompt<256, FMT, SCORED>(a, s);
 }
 
-// Scratch for the parts of any call of so many tiles or fewer (fewer tiles are split more often): heads * splits is below kSplitBlocks + heads.
+// Scratch for the parts of any call of so many heads' tiles (of the least size) or fewer: fewer tiles are split more often, but a call has fewer parts
+// than kSplitBlocks and its tiles together, and one that splits has fewer tiles than kSplitBlocks.
 static size_t prompt_scratch_bytes(const paro_kv_cache &c, int64_t tiles)
 {
-    const int64_t heads = tiles * c.kv_heads, parts = heads < 2 * kSplitBlocks / kMaxSplits ? heads * kMaxSplits : 2 * kSplitBlocks;
-    return (sizeof(float) * kTilePairs * (c.head_dim + 2) * (size_t)parts + 255) / 256 * 256;
+    const int64_t heads = tiles * c.kv_heads, parts = heads * kMaxSplits < kMostParts ? heads * kMaxSplits : kMostParts;
+    const int pairs = c.head_dim == 256 ? Shapes<256>::Many::Pairs : Shapes<128>::Many::Pairs;
+    return (sizeof(float) * pairs * (c.head_dim + 2) * (size_t)parts + 255) / 256 * 256;
 }
+constexpr int kLeastPairs = 32;                  // of a tile in any shape
 
 }  // namespace paro
 
@@ -573,7 +811,7 @@ extern "C" size_t paro_workspace_exchange_bytes_prompt(const paro_kv_cache *cach
 {
     using namespace paro;
     if (!cache || cache->kv_heads <= 0 || q_heads <= 0 || q_heads % cache->kv_heads || T <= 0 || batch <= 0) return 0;
-    const size_t counters = (size_t)prompt_tiles(T, q_heads / cache->kv_heads, batch) * cache->kv_heads * sizeof(uint32_t);
+    const size_t counters = (size_t)prompt_tiles(T, q_heads / cache->kv_heads, batch, kLeastPairs) * cache->kv_heads * sizeof(uint32_t);
     return kWsPartialOff + (counters + 255) / 256 * 256;
 }
 
@@ -581,7 +819,7 @@ extern "C" size_t paro_workspace_bytes_prompt(const paro_kv_cache *cache, int32_
 {
     using namespace paro;
     const size_t e = paro_workspace_exchange_bytes_prompt(cache, q_heads, T, batch);
-    return e && cache->head_dim > 0 ? e + prompt_scratch_bytes(*cache, prompt_tiles(T, q_heads / cache->kv_heads, batch)) : 0;
+    return e && cache->head_dim > 0 ? e + prompt_scratch_bytes(*cache, prompt_tiles(T, q_heads / cache->kv_heads, batch, kLeastPairs)) : 0;
 }
 
 extern "C" paro_status paro_prompt_attention(const paro_kv_cache *cache, const paro_half_t *Q, int64_t ldq, int32_t q_heads, int32_t T,
@@ -604,8 +842,8 @@ extern "C" paro_status paro_prompt_attention(const paro_kv_cache *cache, const p
     // a sequence's tokens and pairs, and the blocks of a launch, are numbered with 32 bits
     const int64_t tokens = (int64_t)table_width * c.page;
     if (q_heads > 65535 || tokens > (int64_t)1 << 30 || T > 1 << 24 || (int64_t)T * q_heads > (int64_t)1 << 30) return PARO_ERR_UNSUPPORTED;
-    const int64_t tiles = prompt_tiles(T, q_heads / c.kv_heads, batch), splits = prompt_splits(tiles, c.kv_heads);
-    if (tiles * c.kv_heads * splits > (int64_t)1 << 24) return PARO_ERR_UNSUPPORTED;       // a launch holds fewer than 2^32 threads
+    const int64_t tiles = prompt_tiles(T, q_heads / c.kv_heads, batch, kLeastPairs);
+    if (tiles * c.kv_heads > (int64_t)1 << 23) return PARO_ERR_UNSUPPORTED;       // a launch holds fewer than 2^32 threads
     if (!ws || ws_bytes < paro_workspace_bytes_prompt(cache, q_heads, T, batch)) return PARO_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return PARO_ERR_ALIGN;
 
@@ -616,7 +854,7 @@ extern "C" paro_status paro_prompt_attention(const paro_kv_cache *cache, const p
     a.partial = (float *)((char *)ws + (ws_bytes & ~(size_t)255) - prompt_scratch_bytes(c, tiles));
     a.ldq = ldq; a.ldo = ldo; a.ld_table = ld_table;
     a.page_log = log2_of(c.page); a.n_pages = c.n_pages; a.kv_heads = c.kv_heads; a.group = q_heads / c.kv_heads; a.width = table_width;
-    a.batch = batch; a.window = window < 1 << 30 ? window : 0; a.T = T; a.tiles = (int)tiles; a.splits = (int)splits;
+    a.batch = batch; a.window = window < 1 << 30 ? window : 0; a.T = T;
     a.scale = scale * kLog2e;
     hipStream_t s = (hipStream_t)stream;
     const bool scored = a.scores.cap > 0 || a.scores.slopes;
