@@ -170,11 +170,12 @@ __device__ inline void prompt_copy(__amdgpu_buffer_rsrc_t r, uint8_t *lds, int o
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (PromptLds *)lds, 16, off, base, 0, 0);
 }
 
-// LDS: keys [tokens/16][head_dim/8][16 tokens] of 16 bytes; values [tokens][head_dim] in blocks of 32 channels whose order in a row depends on
-// the row, so that the transposed reads of 4 rows at once fall on distinct banks.
+// LDS: keys [tokens/16][head_dim/8][16 tokens] of 16 bytes; values [tokens][head_dim] in 16-byte units whose order in a row depends on
+// the row: transposed reads take 64 bytes of 4 rows at once, writes of converted values every other or every 4th unit of a few rows, and both fall on
+// distinct banks.
 template <int D> __device__ inline int key_at(int t, int unit) { return ((t >> 4) * (D / 8) + unit) * 256 + (t & 15) * 16; }
-template <int D> __device__ inline int value_block(int t, int block) { return D == 64 ? block ^ ((t >> 1) & 1) : block ^ (t & 3); }
-template <int D> __device__ inline int value_at(int t, int c) { return t * 2 * D + value_block<D>(t, c >> 5) * 64 + (c & 31) * 2; }
+template <int D> __device__ inline int value_unit(int t, int unit) { return D == 64 ? unit ^ (5 * ((t >> 1) & 1)) : unit ^ (5 * (t & 3)) ^ (D == 256 ? 2 * (unit >> 4) : 0); }
+template <int D> __device__ inline int value_at(int t, int c) { return t * 2 * D + value_unit<D>(t, c >> 3) * 16 + (c & 7) * 2; }
 
 // 16 tokens of keys or of values on a page, from the page's memory to LDS: fp16 caches' without a way through registers, others' through x.
 template <int D, int FMT, bool KEYS>
@@ -200,7 +201,7 @@ struct Run {
         }
         if constexpr (FMT == kFp16) {            // the 16 bytes that come to 16 (lane + 64 i) of the run in LDS
             const int to = (lane + 64 * i) * 16, t = to / (2 * D);
-            return t * 2 * D + value_block<D>(t, to % (2 * D) / 64) * 64 + to % 64;
+            return t * 2 * D + value_unit<D>(t, to % (2 * D) / 16) * 16;
         }
         return (lane + 64 * i) * M::Bytes;
     }
@@ -274,14 +275,22 @@ template <class S, int FMT, bool SCORED>
 __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_kernel(const PromptArgs a)
 {
     constexpr int D = S::D, NB = S::NB, R = D / 32, KS = D / 16;       // channel tiles of the result, steps of the first product
-    extern __shared__ __attribute__((aligned(16))) uint8_t s_tiles[];        // keys [2], values [2]; later the waves' results
+    // Two tiles of keys and two of values; later the waves' results, one wave's to a tile's place.  They are objects of their own, and a round knows
+    // which ones it reads and which it fills: the compiler makes a read wait for every copy to LDS that might be to the same object.
+    __shared__ __attribute__((aligned(16))) uint8_t s_keys0[S::TileBytes], s_keys1[S::TileBytes], s_values0[S::TileBytes], s_values1[S::TileBytes];
+    const auto place = [&](int i) { return i == 0 ? s_keys0 : i == 1 ? s_keys1 : i == 2 ? s_values0 : s_values1; };
     __shared__ int s_lo[kWaves][2], s_hi[kWaves][2];
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, n32 = lane & 31, wm = wave % S::WM, wn = wave / S::WM;
 
-    // longest tiles first; the heads of a tile side by side, which puts a head on one XCD where there are 8 of them
-    const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
+    // The heads of a tile side by side, which puts a head on one XCD where there are 8 of them; longest tiles first.  Where all blocks are on the chip
+    // at once, those that come second to a compute unit begin with the shortest, so that it has a long and a short one.
+    const int slots = kChip / a.kv_heads, all = a.tiles * a.splits;
+    int rest = blockIdx.x / a.kv_heads;
+    const int head = blockIdx.x - rest * a.kv_heads;
+    if (S::Blocks == 2 && rest >= slots && all <= 2 * slots) rest = all - 1 - (rest - slots);
+    const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
     Where w;
     int work;
     if (!find_tile<S>(w, work, a, tile, lane)) return;
@@ -348,6 +357,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[r][j] = 0;
+    bool far = false;                            // a maximum of the wave's is beyond kFarMax
     float m = -INFINITY, l = 0, up = scale, off = kShift;       // p = 2^(up s + off) of a score s is taken from the maximum m; l over this lane's tokens only
 
     // The pages of 64 runs of 16 tokens from run0 on, one to a lane (-1: not there, or past the part's tokens), and which of them are there.
@@ -366,16 +376,13 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         there = __ballot(pages >= 0);
     };
     struct Pages { int page[S::Quarters]; uint32_t gone; };      // of this wave's runs of a tile; a bit for every run of the tile that is not there
-    const auto pages_of = [&](int u) {
-        if (u * Runs - run0 >= 64) turn(u * Runs);
+    const auto pages_of = [&](int u) {           // once turn() has got them
         Pages p;
 #pragma unroll
         for (int i = 0; i < S::Quarters; ++i) p.page[i] = __builtin_amdgcn_readlane(pages, u * Runs - run0 + wave + 4 * i);
         p.gone = (uint32_t)(~(there >> (u * Runs - run0))) & ((1u << Runs) - 1);
         return p;
     };
-    const auto keys_of = [&](int u) { return s_tiles + (u & 1) * S::TileBytes; };
-    const auto values_of = [&](int u) { return s_tiles + (2 + (u & 1)) * S::TileBytes; };
     constexpr int Loads = Move<D, FMT>::Loads, Jobs = S::Quarters * Loads;       // requests of a wave for its share of a tile's keys, and of its values
     constexpr bool Copied = FMT == kFp16;
     Run<D, FMT, true> kr[S::Quarters];
@@ -390,8 +397,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
 #pragma unroll
         for (int i = 0; i < S::Quarters; ++i) vr[i].at(a, head, p.page[i], u * S::Tokens + (wave + 4 * i) * 16);
     };
-    const auto key_run = [&](int u, int job) { return keys_of(u) + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
-    const auto value_run = [&](int u, int job) { return values_of(u) + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
+    const auto run_in = [&](uint8_t *place, int job) { return place + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
 
     // S^T of a tile: score j of block b is of token 32 (NB wn + b) + 8 (j / 4) + 4 h + j % 4
     F16 s[NB];
@@ -439,21 +445,22 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) acc[r][j] *= f;
+            const float ref = m == -INFINITY ? 0.0f : m;
+            far = __ballot(fabsf(ref) > kFarMax) != 0;
+            up = far ? 1.0f : scale;
+            off = far ? kShift : kShift - ref;
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        up = scale;
-        off = kShift - ref;
-        if (__ballot(fabsf(ref) > kFarMax)) {
+        if (far) {
             // product and difference as one would be off by up to half a unit of the maximum here, and p has to stay within fp16
+            const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
+#pragma clang fp contract(off)
                     const float y = z[b][j] * scale;
                     z[b][j] = y - ref;
                 }
-            up = 1.0f;
-            off = kShift;
         }
     };
 
@@ -466,12 +473,14 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             values_at(p0, u0);
             if constexpr (Copied) {
 #pragma unroll
-                for (int i = 0; i < Jobs; ++i) kr[i / Loads].copy(key_run(u0, i), i % Loads, lane, a.page_log);
+                for (int i = 0; i < Jobs; ++i) kr[i / Loads].copy(run_in(s_keys0, i), i % Loads, lane, a.page_log);
 #pragma unroll
-                for (int i = 0; i < Jobs; ++i) vr[i / Loads].copy(value_run(u0, i), i % Loads, lane, a.page_log);
+                for (int i = 0; i < Jobs; ++i) vr[i / Loads].copy(run_in(s_values0, i), i % Loads, lane, a.page_log);
                 keys_at(p1, u0 + 1);
 #pragma unroll
-                for (int i = 0; i < Jobs; ++i) kr[i / Loads].copy(key_run(u0 + 1, i), i % Loads, lane, a.page_log);
+                for (int i = 0; i < Jobs; ++i) kr[i / Loads].copy(run_in(s_keys1, i), i % Loads, lane, a.page_log);
+                values_at(p1, u0 + 1);
+                keys_at(p2, u0 + 2);
                 prompt_wait_vm<0>();
             } else {
 #pragma unroll
@@ -481,24 +490,24 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 keys_at(p1, u0 + 1);
 #pragma unroll
                 for (int i = 0; i < Jobs; ++i) {
-                    kr[0].put(kh[i], key_run(u0, i), i % Loads, lane);
+                    kr[0].put(kh[i], run_in(s_keys0, i), i % Loads, lane);
                     kr[i / Loads].ask(kh[i], i % Loads, lane, a.page_log);
                 }
                 values_at(p1, u0 + 1);
 #pragma unroll
                 for (int i = 0; i < Jobs; ++i) {
-                    vr[0].put(vh[i], value_run(u0, i), i % Loads, lane);
+                    vr[0].put(vh[i], run_in(s_values0, i), i % Loads, lane);
                     vr[i / Loads].ask(vh[i], i % Loads, lane, a.page_log);
                 }
                 keys_at(p2, u0 + 2);
 #pragma unroll
                 for (int i = 0; i < Jobs; ++i) {
-                    kr[0].put(kh[i], key_run(u0 + 1, i), i % Loads, lane);
+                    kr[0].put(kh[i], run_in(s_keys1, i), i % Loads, lane);
                     kr[i / Loads].ask(kh[i], i % Loads, lane, a.page_log);
                 }
             }
             __syncthreads();
-            const uint8_t *keys = keys_of(u0);
+            const uint8_t *keys = s_keys0;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -516,8 +525,10 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         // A round has the scores of tile u.  It turns them into weights while the matrix cores compute those of u + 1, then multiplies the weights
         // with the values of u while it looks for the next maximum; keys of u + 2 and values of u + 1 go to LDS meanwhile.  What the vector units do is dealt
         // out over the matrix instructions evenly, 32 cycles of a matrix core to as many of a vector unit: 8 each for the issue and for an exponential, 4 for others.
-        for (int u = u0; u < u1; ++u) {
-            uint8_t *values = values_of(u);
+        const auto round = [&](int u, uint8_t *free_keys, uint8_t *keys, uint8_t *values, uint8_t *free_values) __attribute__((always_inline)) {
+            constexpr int Ahead = NB * KS < 5 ? NB * KS : 5;         // operands on their way from LDS, which takes 130 cycles and more
+            half8v f[Ahead + 1];
+            each<0, Ahead>([&](auto at) { f[at] = key_frag(keys, at); });
             if (u * S::Tokens < whole_lo || (u + 1) * S::Tokens > whole_hi) {
                 // A tile that some pair does not see all of: values that nobody sees become zeros, for such places may hold NaN, whose product with a weight
                 // of 0 is not 0.  Others that are not finite are taken here by the pairs that see them (their results are not finite, whatever the
@@ -552,17 +563,14 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 }
             }
             const uint32_t gone = p1.gone;
-            if constexpr (Copied) {              // keys of u + 2, values of u + 1; past the part's last tile there is nothing to read, and zeros come
-                values_at(p1, u + 1);
-                keys_at(p2, u + 2);
-                p1 = p2;
-                p2 = pages_of(u + 3);
-            } else {                             // those are held, and are put down before the next are asked for
+            if ((u + 3) * Runs - run0 >= 64) turn((u + 3) * Runs);
+            // the runs that are copied or asked for next: keys of u + 3, values of u + 2; past the part's last tile there is nothing to read, and zeros come
+            const auto advance = [&]() {
                 values_at(p2, u + 2);
                 p1 = p2;
                 p2 = pages_of(u + 3);
                 keys_at(p2, u + 3);
-            }
+            };
 
             constexpr int All = NB * 8, Late = NB * 3;       // pairs of scores; those whose weights the second product does not need at once
             half8v p[2 * NB];
@@ -579,48 +587,48 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             F16 next[NB];
             {
                 constexpr int Steps = NB * KS;
-                const uint8_t *keys = keys_of(u + 1);
-                half8v f[3] = {key_frag(keys, 0), key_frag(keys, 1)};
                 each<0, Steps>([&](auto at) {
                     constexpr int i = at;
-                    if constexpr (i + 2 < Steps) f[(i + 2) % 3] = key_frag(keys, i + 2);
+                    if constexpr (i + Ahead < Steps) f[(i + Ahead) % (Ahead + 1)] = key_frag(keys, i + Ahead);
+                    else f[(i + Ahead) % (Ahead + 1)] = value_frag(values, i + Ahead - Steps);
                     F16 z = next[i / KS];
                     if constexpr (i % KS == 0)
 #pragma unroll
                         for (int j = 0; j < 16; ++j) z[j] = 0;
-                    next[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % 3], q[i % KS], z, 0, 0, 0);
+                    next[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % (Ahead + 1)], q[i % KS], z, 0, 0, 0);
                     if constexpr (Copied)
                         each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) {
                             constexpr int k = job;
-                            if constexpr (k < Jobs) kr[k / Loads].copy(key_run(u + 2, k), k % Loads, lane, a.page_log);
-                            else vr[(k - Jobs) / Loads].copy(value_run(u + 1, k - Jobs), (k - Jobs) % Loads, lane, a.page_log);
+                            if constexpr (k < Jobs) kr[k / Loads].copy(run_in(free_keys, k), k % Loads, lane, a.page_log);
+                            else vr[(k - Jobs) / Loads].copy(run_in(free_values, k - Jobs), (k - Jobs) % Loads, lane, a.page_log);
                         });
                     each<i *(All - Late) / Steps, (i + 1) * (All - Late) / Steps>(weigh);
+                    if constexpr (!Copied && i == Steps / 2) advance();
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
             finish(next, u + 1, gone);
             float top = -INFINITY;
             {
-                constexpr int Steps = 2 * NB * R, Soon = NB * R;
-                half8v f[3] = {value_frag(values, 0), value_frag(values, 1)};
+                constexpr int Steps = 2 * NB * R, Soon = NB * R, Before = NB * KS;      // of the first product, whose ring of operands goes on
                 each<0, Steps>([&](auto at) {
                     constexpr int i = at;
-                    if constexpr (i + 2 < Steps) f[(i + 2) % 3] = value_frag(values, i + 2);
-                    acc[i % R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % 3], p[i / R], acc[i % R], 0, 0, 0);
+                    if constexpr (i + Ahead < Steps) f[(Before + i + Ahead) % (Ahead + 1)] = value_frag(values, i + Ahead);
+                    acc[i % R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[(Before + i) % (Ahead + 1)], p[i / R], acc[i % R], 0, 0, 0);
                     if constexpr (i < Soon) each<All - Late + i * Late / Soon, All - Late + (i + 1) * Late / Soon>(weigh);
                     each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) {
                         constexpr int c = two;
                         top = max3(top, next[c / 8][2 * (c % 8)], next[c / 8][2 * (c % 8) + 1]);
                     });
+                    if constexpr (Copied && i == Steps / 2) advance();
                     if constexpr (!Copied)
                         each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) {
                             constexpr int k = job;
                             if constexpr (k < Jobs) {
-                                kr[0].put(kh[k], key_run(u + 2, k), k % Loads, lane);
+                                kr[0].put(kh[k], run_in(free_keys, k), k % Loads, lane);
                                 kr[k / Loads].ask(kh[k], k % Loads, lane, a.page_log);
                             } else {
-                                vr[0].put(vh[k - Jobs], value_run(u + 1, k - Jobs), (k - Jobs) % Loads, lane);
+                                vr[0].put(vh[k - Jobs], run_in(free_values, k - Jobs), (k - Jobs) % Loads, lane);
                                 vr[(k - Jobs) / Loads].ask(vh[k - Jobs], (k - Jobs) % Loads, lane, a.page_log);
                             }
                         });
@@ -632,20 +640,24 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             follow(top, s);
             if constexpr (Copied) prompt_wait_vm<0>();
             __syncthreads();
+        };
+        for (int u = u0; u < u1; u += 2) {
+            round(u, s_keys0, s_keys1, s_values0, s_values1);
+            if (u + 1 < u1) round(u + 1, s_keys1, s_keys0, s_values1, s_values0);
         }
     }
     l = sum2(l);
 
     if constexpr (S::WN > 1) {
         // the waves that share pairs: their results meet in LDS, and each finishes every WN-th run of 4 registers
-        float *sums = (float *)s_tiles;          // [wave][R][4][64] of 4
+        static_assert(R * 4 * 64 * 16 <= S::TileBytes, "a wave's results fit a tile's place");      // [R][4][64] of 4
         __shared__ float s_m[kWaves][32], s_l[kWaves][32];
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(F4 *)(sums + (((wave * R + r) * 4 + i) * 64 + lane) * 4) = F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]};
+                *(F4 *)(place(wave) + ((r * 4 + i) * 64 + lane) * 16) = F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]};
         if (h == 0) { s_m[wave][n32] = m; s_l[wave][n32] = l; }
         __syncthreads();
         float f[S::WN];
@@ -663,11 +675,11 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (i % S::WN != wn) continue;
+                if (i >= 4 / S::WN) continue;
                 F4 y = {0, 0, 0, 0};
 #pragma unroll
                 for (int z = 0; z < S::WN; ++z) {
-                    const F4 v = *(const F4 *)(sums + ((((wm + z * S::WM) * R + r) * 4 + i) * 64 + lane) * 4);
+                    const F4 v = *(const F4 *)(place(wm + z * S::WM) + ((r * 4 + i * S::WN + wn) * 64 + lane) * 16);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[e] = fmaf(v[e], f[z], y[e]);
                 }
@@ -675,8 +687,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 for (int e = 0; e < 4; ++e) acc[r][4 * i + e] = y[e];
             }
     }
-    const auto mine = [&](int i) { return S::WN == 1 || i % S::WN == wn; };      // runs of 4 registers that this wave finishes
-
+    // from here on a wave has runs i * WN + wn of the 4 registers of a channel tile, in registers 4 i ..
     if (parts > 1) {
         // every part's m, l and sums where its lanes left them, through memory that all XCDs see
         const size_t tile_at = (size_t)tile * a.kv_heads + head;
@@ -691,10 +702,9 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (mine(i))
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]}), to, sums_at(r, i), 0,
-                                                               kPromptAgent);
+                for (int i = 0; i < 4 / S::WN; ++i)
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(B4, F4{acc[r][4 * i], acc[r][4 * i + 1], acc[r][4 * i + 2], acc[r][4 * i + 3]}), to,
+                                                           sums_at(r, i * S::WN + wn), 0, kPromptAgent);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -706,45 +716,75 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         }
         __syncthreads();
         if (!__builtin_amdgcn_readfirstlane(s_last)) return;
+        // as many parts as registers hold at a time, all of their requests before the first use; a part that is not there gives zeros, and does not count
+        constexpr int At = 8 * S::WN / R < 1 ? 1 : 8 * S::WN / R > 8 ? 8 : 8 * S::WN / R;
         m = -INFINITY;
-        for (int p = 0; p < parts; ++p) m = fmaxf(m, __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part_rsrc(p), ml_at, 0, kPromptAgent)));
-        const float ref = m == -INFINITY ? 0.0f : m;
         l = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[r][j] = 0;
-        for (int p = 0; p < parts; ++p) {
-            const __amdgpu_buffer_rsrc_t from = part_rsrc(p);
-            const U2 ml = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(from, ml_at, 0, kPromptAgent));
-            F4 y[R][4];
+        for (int p0 = 0; p0 < parts; p0 += At) {
+            U2 ml[At];
+            F4 y[At][R][4 / S::WN];
+            const auto from = [&](int z) { return prompt_rsrc(a.partial + (tile_at * a.splits + p0 + z) * S::PartFloats, p0 + z < parts ? (uint32_t)(S::PartFloats * 4) : 0); };
+#pragma unroll
+            for (int z = 0; z < At; ++z) ml[z] = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(from(z), ml_at, 0, kPromptAgent));
+#pragma unroll
+            for (int z = 0; z < At; ++z)
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4 / S::WN; ++i) y[z][r][i] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(from(z), sums_at(r, i * S::WN + wn), 0, kPromptAgent));
+            float top = m;
+#pragma unroll
+            for (int z = 0; z < At; ++z) top = fmaxf(top, p0 + z < parts ? __uint_as_float(ml[z][0]) : -INFINITY);
+            const float ref = top == -INFINITY ? 0.0f : top, keep = __builtin_amdgcn_exp2f(m - ref);
+            m = top;
+            l *= keep;
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (mine(i)) y[r][i] = __builtin_bit_cast(F4, __builtin_amdgcn_raw_buffer_load_b128(from, sums_at(r, i), 0, kPromptAgent));
-            const float f = __builtin_amdgcn_exp2f(__uint_as_float(ml[0]) - ref);
-            l = fmaf(__uint_as_float(ml[1]), f, l);
+                for (int j = 0; j < 16; ++j) acc[r][j] *= keep;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int z = 0; z < At; ++z) {
+                const float f = p0 + z < parts ? __builtin_amdgcn_exp2f(__uint_as_float(ml[z][0]) - ref) : 0.0f;
+                l = fmaf(__uint_as_float(ml[z][1]), f, l);
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (mine(j >> 2)) acc[r][j] = fmaf(y[r][j >> 2][j & 3], f, acc[r][j]);
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4 / S::WN; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][4 * i + e] = fmaf(y[z][r][i][e], f, acc[r][4 * i + e]);
+            }
         }
     }
 
-    if (pair < pairs) {
+    if (pair < pairs && a.lse && h == 0 && wn == 0)
+        a.lse[(int64_t)(w.row0 + row) * (a.kv_heads * a.group) + qhead] = l == 0.0f ? -INFINITY : (m - kShift + __builtin_amdgcn_logf(l)) * kLn2;
+    // Results go by way of LDS, so that a row's channels are written side by side (as they lie in registers, 16 bytes of 32 rows at a time, a block
+    // took up to 20000 cycles for them): [32 pairs][D], 8 bytes more a row so that rows fall on other banks.
+    {
         const float inv = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-        _Float16 *o = a.o + (int64_t)(w.row0 + row) * a.ldo + (int64_t)qhead * D + 4 * h;
+        constexpr int Row = 2 * D + 8;
+        static_assert(32 * Row <= S::TileBytes, "32 pairs' results fit a tile's place");
+        uint8_t *out = place(wm);
+        __syncthreads();                         // LDS is free: the waves' sums have been read
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (mine(i))
-                    *(half4v *)(o + 32 * r + 8 * i) = half4v{(_Float16)(acc[r][4 * i] * inv), (_Float16)(acc[r][4 * i + 1] * inv), (_Float16)(acc[r][4 * i + 2] * inv),
-                                                           (_Float16)(acc[r][4 * i + 3] * inv)};
-        if (a.lse && h == 0 && wn == 0)
-            a.lse[(int64_t)(w.row0 + row) * (a.kv_heads * a.group) + qhead] = l == 0.0f ? -INFINITY : (m - kShift + __builtin_amdgcn_logf(l)) * kLn2;
+            for (int i = 0; i < 4 / S::WN; ++i)
+                *(half4v *)(out + n32 * Row + (32 * r + 8 * (i * S::WN + wn) + 4 * h) * 2) =
+                    half4v{(_Float16)(acc[r][4 * i] * inv), (_Float16)(acc[r][4 * i + 1] * inv), (_Float16)(acc[r][4 * i + 2] * inv), (_Float16)(acc[r][4 * i + 3] * inv)};
+        __syncthreads();
+        constexpr int Lanes = D / 4;             // of a row, 8 bytes each
+#pragma unroll 4
+        for (int i = tid; i < S::Pairs * Lanes; i += kPromptThreads) {
+            const int p = i / Lanes, c = i % Lanes * 4;
+            if (w.pair0 + p >= pairs) break;
+            const int to = (w.pair0 + p) / a.group, of = head * a.group + w.pair0 + p - to * a.group;
+            *(half4v *)(a.o + (int64_t)(w.row0 + to) * a.ldo + (int64_t)of * D + c) = *(const half4v *)(place(p >> 5) + (p & 31) * Row + c * 2);
+        }
     }
 }
 
@@ -771,16 +811,9 @@ constexpr int kFewPairs = 64;                    // of a sequence on average, up
 template <class S, int FMT, bool SCORED>
 static hipError_t launch_prompt(PromptArgs &a, hipStream_t s)
 {
-    constexpr int lds = 4 * S::TileBytes;
-    static std::atomic<uint64_t> attr_done{0};
-    if (const int dev = once_pending(attr_done); dev >= 0) {
-        const hipError_t e = hipFuncSetAttribute((const void *)prompt_attention_kernel<S, FMT, SCORED>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-        once_done(attr_done, dev);
-    }
     a.tiles = (int)prompt_tiles(a.T, a.group, a.batch, S::Pairs);
     a.splits = (int)prompt_splits(a.tiles, a.kv_heads);
-    hipLaunchKernelGGL((prompt_attention_kernel<S, FMT, SCORED>), dim3((unsigned)(a.tiles * a.kv_heads * a.splits)), dim3(kPromptThreads), lds, s, a);
+    hipLaunchKernelGGL((prompt_attention_kernel<S, FMT, SCORED>), dim3((unsigned)(a.tiles * a.kv_heads * a.splits)), dim3(kPromptThreads), 0, s, a);
     return hipGetLastError();
 }
 template <int D, int FMT, bool SCORED>

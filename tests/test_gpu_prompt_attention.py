@@ -62,6 +62,16 @@ def test_lengths(P, fmt, hq, hkv, D, page):
     check(P, *filled(P, lengths, hkv, D, page, fmt, hq + D), new, lengths, hq)
 
 
+@pytest.mark.parametrize("fmt", ["fp16", "e4m3", "mxfp4"])
+@pytest.mark.parametrize("hq,hkv,D,page", [(2, 2, 64, 16), (5, 1, 128, 32), (8, 1, 256, 16)])
+def test_few_rows(P, fmt, hq, hkv, D, page):
+    say(f"few rows of many sequences, {fmt} {hq}/{hkv} x {D}, page {page}")
+    new = [1, 3, 0, 7, 5, 2, 1, 4, 6, 1, 2, 3]
+    lengths = [1, 3, 0, 7, 33, 64, 65, 127, 128, 129, 300, 1500]
+    check(P, *filled(P, lengths, hkv, D, page, fmt, hq + D), new, lengths, hq)
+    check(P, *filled(P, lengths, hkv, D, page, fmt, hq + D), new, lengths, hq, window=50, cap=9.0)
+
+
 @pytest.mark.parametrize("fmt,D,hq,hkv,new,held", [("fp16", 128, 8, 2, 200, 0), ("fp16", 128, 8, 2, 5, 5003), ("mxfp4", 128, 4, 1, 3, 20011), ("e4m3", 64, 16, 1, 9, 9001),
                                                    ("fp16", 256, 4, 2, 67, 4000), ("mxfp4", 256, 4, 2, 1, 4001), ("fp16", 64, 2, 2, 513, 500)])
 def test_long(P, fmt, D, hq, hkv, new, held):
