@@ -296,24 +296,44 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     if (!find_tile<S>(w, work, a, tile, lane)) return;
     const int pairs = w.rows * a.group, pair = w.pair0 + wm * 32 + n32;
     // the pair's row and query head (the last pair's for lanes past it)
+    const auto lo_of = [&](int p) { const int lo = a.window ? p - a.window + 1 : 0; return lo > 0 ? lo : 0; };
+    int prefix = 0;
+    if (a.prefix) { prefix = __builtin_amdgcn_readfirstlane(a.prefix[w.b]); prefix = prefix < w.n ? prefix : w.n; }
+    const auto hi_of = [&](int p) { return p + 1 > prefix ? p + 1 : prefix; };
     const int row = (pair < pairs ? pair : pairs - 1) / a.group, qhead = head * a.group + (pair < pairs ? pair : pairs - 1) - row * a.group;
 
     // what the pair sees: lo <= t < hi, from position pos
     const int pos = w.n - w.rows + row;
-    int lo = 0, hi = pos + 1;
-    if (a.window) lo = pos - a.window + 1;
+    int lo = lo_of(pos), hi = hi_of(pos);
     if (a.first) { const int f = a.first[w.row0 + row]; lo = lo > f ? lo : f; }
-    if (a.prefix) { int f = a.prefix[w.b]; f = f < w.n ? f : w.n; hi = hi > f ? hi : f; }
-    lo = lo > 0 ? lo : 0;
     if (lo >= hi) { lo = INT32_MAX; hi = 0; }
-    int least = lo, most = hi, lo_most = lo, hi_least = hi;     // of the wave; then of the block
+    // The least and largest lo and hi of the block, and the largest lo and least hi of it and of the wave.  Both rise with the row, unless documents have it otherwise.
+    int begin, end, whole_lo, whole_hi, lo_most, hi_least;
+    if (!a.first) {
+        const auto pos_at = [&](int p) { return w.n - w.rows + (p < pairs ? p : pairs - 1) / a.group; };
+        const int p0 = pos_at(w.pair0), p1 = pos_at(w.pair0 + S::Pairs - 1), w0 = pos_at(w.pair0 + wm * 32), w1 = pos_at(w.pair0 + wm * 32 + 31);
+        begin = lo_of(p0); end = hi_of(p1); whole_lo = lo_of(p1); whole_hi = hi_of(p0);
+        lo_most = lo_of(w1); hi_least = hi_of(w0);
+    } else {
+        int least = lo, most = hi;
+        lo_most = lo; hi_least = hi;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        least = min(least, __shfl_xor(least, d)); most = max(most, __shfl_xor(most, d));
-        lo_most = max(lo_most, __shfl_xor(lo_most, d)); hi_least = min(hi_least, __shfl_xor(hi_least, d));
+        for (int d = 1; d < 32; d <<= 1) {
+            least = min(least, __shfl_xor(least, d)); most = max(most, __shfl_xor(most, d));
+            lo_most = max(lo_most, __shfl_xor(lo_most, d)); hi_least = min(hi_least, __shfl_xor(hi_least, d));
+        }
+        lo_most = __builtin_amdgcn_readfirstlane(lo_most); hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+        if (lane == 0) { s_lo[wave][0] = least; s_lo[wave][1] = lo_most; s_hi[wave][0] = most; s_hi[wave][1] = hi_least; }
+        __syncthreads();
+        begin = s_lo[0][0]; end = s_hi[0][0]; whole_lo = s_lo[0][1]; whole_hi = s_hi[0][1];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) {
+            begin = min(begin, s_lo[i][0]); end = max(end, s_hi[i][0]);
+            whole_lo = max(whole_lo, s_lo[i][1]); whole_hi = min(whole_hi, s_hi[i][1]);
+        }
+        begin = __builtin_amdgcn_readfirstlane(begin); end = __builtin_amdgcn_readfirstlane(end);
+        whole_lo = __builtin_amdgcn_readfirstlane(whole_lo); whole_hi = __builtin_amdgcn_readfirstlane(whole_hi);
     }
-    lo_most = __builtin_amdgcn_readfirstlane(lo_most); hi_least = __builtin_amdgcn_readfirstlane(hi_least);
-    if (lane == 0) { s_lo[wave][0] = least; s_lo[wave][1] = lo_most; s_hi[wave][0] = most; s_hi[wave][1] = hi_least; }
 
     // its query: channels 16 s + 8 h ..  A negative scale goes into the queries' sign, a scale of 0 makes them 0: factors of maxima are positive.
     half8v q[KS];
@@ -329,15 +349,6 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     const float scale = SCORED ? 1.0f : a.scale == 0 ? 1.0f : fabsf(a.scale);
     float slope = 0;
     if constexpr (SCORED) if (a.scores.slopes) slope = a.scores.slopes[qhead] * kLog2e;
-    __syncthreads();
-    int begin = s_lo[0][0], end = s_hi[0][0], whole_lo = s_lo[0][1], whole_hi = s_hi[0][1];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) {
-        begin = min(begin, s_lo[i][0]); end = max(end, s_hi[i][0]);
-        whole_lo = max(whole_lo, s_lo[i][1]); whole_hi = min(whole_hi, s_hi[i][1]);
-    }
-    begin = __builtin_amdgcn_readfirstlane(begin); end = __builtin_amdgcn_readfirstlane(end);
-    whole_lo = __builtin_amdgcn_readfirstlane(whole_lo); whole_hi = __builtin_amdgcn_readfirstlane(whole_hi);
     // tiles of tokens, and this split's share of them: parts are as long as a block's share of all work
     const int tile0 = begin < end ? begin / S::Tokens : 0, tiles = begin < end ? (end + S::Tokens - 1) / S::Tokens - tile0 : 0;
     int parts = 1;
@@ -466,7 +477,9 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
 
     if (u0 < u1) {
         turn(run0);
-        Pages p1 = pages_of(u0 + 1), p2 = pages_of(u0 + 2);
+        // A round's requests are for keys of u + Lead and values of u + Lead - 1: at once on the way to LDS, or held for a round.
+        constexpr int Lead = Copied ? 2 : 3;
+        Pages p1 = pages_of(u0 + 1), p2 = pages_of(u0 + 2), p3 = pages_of(u0 + 3);
         {
             const Pages p0 = pages_of(u0);
             keys_at(p0, u0);
@@ -505,6 +518,8 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                     kr[0].put(kh[i], run_in(s_keys1, i), i % Loads, lane);
                     kr[i / Loads].ask(kh[i], i % Loads, lane, a.page_log);
                 }
+                values_at(p2, u0 + 2);
+                keys_at(p3, u0 + 3);
             }
             __syncthreads();
             const uint8_t *keys = s_keys0;
@@ -563,13 +578,14 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 }
             }
             const uint32_t gone = p1.gone;
-            if ((u + 3) * Runs - run0 >= 64) turn((u + 3) * Runs);
-            // the runs that are copied or asked for next: keys of u + 3, values of u + 2; past the part's last tile there is nothing to read, and zeros come
+            if ((u + 4) * Runs - run0 >= 64) turn((u + 4) * Runs);
+            // the next round's requests; past the part's last tile there is nothing to read, and zeros come
             const auto advance = [&]() {
-                values_at(p2, u + 2);
+                values_at(Copied ? p2 : p3, u + Lead);
                 p1 = p2;
-                p2 = pages_of(u + 3);
-                keys_at(p2, u + 3);
+                p2 = p3;
+                p3 = pages_of(u + 4);
+                keys_at(Copied ? p2 : p3, u + Lead + 1);
             };
 
             constexpr int All = NB * 8, Late = NB * 3;       // pairs of scores; those whose weights the second product does not need at once
@@ -603,7 +619,12 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                             else vr[(k - Jobs) / Loads].copy(run_in(free_values, k - Jobs), (k - Jobs) % Loads, lane, a.page_log);
                         });
                     each<i *(All - Late) / Steps, (i + 1) * (All - Late) / Steps>(weigh);
-                    if constexpr (!Copied && i == Steps / 2) advance();
+                    if constexpr (!Copied)
+                        each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) {
+                            constexpr int k = job;
+                            kr[0].put(kh[k], run_in(free_keys, k), k % Loads, lane);
+                            kr[k / Loads].ask(kh[k], k % Loads, lane, a.page_log);
+                        });
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
@@ -620,18 +641,13 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                         constexpr int c = two;
                         top = max3(top, next[c / 8][2 * (c % 8)], next[c / 8][2 * (c % 8) + 1]);
                     });
-                    if constexpr (Copied && i == Steps / 2) advance();
                     if constexpr (!Copied)
-                        each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) {
+                        each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) {
                             constexpr int k = job;
-                            if constexpr (k < Jobs) {
-                                kr[0].put(kh[k], run_in(free_keys, k), k % Loads, lane);
-                                kr[k / Loads].ask(kh[k], k % Loads, lane, a.page_log);
-                            } else {
-                                vr[0].put(vh[k - Jobs], run_in(free_values, k - Jobs), (k - Jobs) % Loads, lane);
-                                vr[(k - Jobs) / Loads].ask(vh[k - Jobs], (k - Jobs) % Loads, lane, a.page_log);
-                            }
+                            vr[0].put(vh[k], run_in(free_values, k), k % Loads, lane);
+                            vr[k / Loads].ask(vh[k], k % Loads, lane, a.page_log);
                         });
+                    if constexpr (i == Steps - 1) advance();
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
