@@ -456,8 +456,8 @@ paro_status paro_paged_attention(const paro_kv_cache *cache, const paro_half_t *
  *      x = cap tanh(scale q_h . k_t / cap) - slopes[h] |p - t|
  * for a query at position p (here p = n - 1): scores that stay within +-cap, a bias that grows with the distance, or both.
  * A score of -inf is -cap under a cap, and its token counts.  cap: 0 (none) or positive, finite, with scale / cap finite
- * (PARO_ERR_SHAPE otherwise).  slopes: device fp32 [q_heads], 4-byte aligned, or NULL (none); finite values.  tanh is off by
- * 2^-22 of itself at most.  scores NULL, or with neither: paro_paged_attention. */
+ * (PARO_ERR_SHAPE otherwise).  slopes: device fp32 [q_heads], 4-byte aligned, or NULL (none); finite values.  Scores are off
+ * by 2^-21 of themselves at most and, with caps up to 64, by 2^-24 of the cap.  scores NULL, or with neither: paro_paged_attention. */
 typedef struct {
     float cap;
     const float *slopes;

@@ -32,7 +32,7 @@ typedef uint32_t U2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4, kPromptThreads = 64 * kWaves;
 constexpr int kMaxSplits = 32;
-constexpr int kSplitBlocks = 512;                // tiles are split while there are fewer of them
+constexpr int kSplitBlocks = 512;               // tiles are split while there are fewer of them
 constexpr int kMostParts = 2 * kSplitBlocks;     // that a call can have
 constexpr int kChip = 256;                       // compute units
 constexpr int kLeastTokens = 256;                // that a part has at least
@@ -238,13 +238,13 @@ struct Run {
 };
 template <int N> __device__ __forceinline__ void prompt_wait_vm() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14)); }
 
-__device__ inline bool any_not_finite(half8v x)
+// The larger magnitudes, as 16-bit numbers, of m's and of 8 fp16 values' (those that are not finite have 0x7c00 and more).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline u16x2 most_magnitude(u16x2 m, U4 x)
 {
-    const U4 u = __builtin_bit_cast(U4, x);
-    bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad |= (u[i] & 0x7c00u) == 0x7c00u || (u[i] & 0x7c000000u) == 0x7c000000u;
-    return bad;
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
+    return m;
 }
 
 typedef __fp16 Tr4 __attribute__((__vector_size__(8)));
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     __shared__ __attribute__((aligned(16))) uint8_t s_keys0[S::TileBytes], s_keys1[S::TileBytes], s_values0[S::TileBytes], s_values1[S::TileBytes];
     const auto place = [&](int i) { return i == 0 ? s_keys0 : i == 1 ? s_keys1 : i == 2 ? s_values0 : s_values1; };
     __shared__ int s_lo[kWaves][2], s_hi[kWaves][2];
-    __shared__ int s_last;
+    __shared__ int s_bad, s_last;                // s_bad: 1 + the tile that has values that are not finite, where not all see them
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, n32 = lane & 31, wm = wave % S::WM, wn = wave / S::WM;
 
@@ -434,15 +434,18 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             for (int b = 0; b < NB; ++b) adjust(z[b], a, slope, pos - t0 - 32 * b);
         }
         if (u * S::Tokens < lo_most || (u + 1) * S::Tokens > hi_least || gone) {
-            const int from = lo - t0, to = hi - t0;
+            // a bit for every token of a block that the pair sees; a score keeps its bits or takes those of -inf
+            const auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t away = gone >> (2 * (NB * wn + b)), there = (away & 1 ? 0u : 0xffffu) | (away & 2 ? 0u : 0xffff0000u);
+                const uint32_t seen = below(hi - t0 - 32 * b) & ~below(lo - t0 - 32 * b) & (there >> (4 * h));
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const int t = 32 * b + 8 * (j >> 2) + (j & 3);
-                    const bool in = t >= from && t < to && !((gone >> (2 * (NB * wn + b) + (j >> 3))) & 1);
-                    z[b][j] = in ? z[b][j] : -INFINITY;
+                    const int in = __builtin_amdgcn_sbfe((int)seen, 8 * (j >> 2) + (j & 3), 1);
+                    z[b][j] = __uint_as_float((__float_as_uint(z[b][j]) & (uint32_t)in) | (0xff800000u & ~(uint32_t)in));
                 }
+            }
         }
     };
     // new scores z, the largest of this lane's `top`: the sums follow if the maximum has grown by more than kSlack
@@ -476,6 +479,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     };
 
     if (u0 < u1) {
+        if (tid == 0) s_bad = 0;
         turn(run0);
         // A round's requests are for keys of u + Lead and values of u + Lead - 1: at once on the way to LDS, or held for a round.
         constexpr int Lead = Copied ? 2 : 3;
@@ -548,15 +552,17 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 // A tile that some pair does not see all of: values that nobody sees become zeros, for such places may hold NaN, whose product with a weight
                 // of 0 is not 0.  Others that are not finite are taken here by the pairs that see them (their results are not finite, whatever the
                 // weight is) before zeros take their place.
-                bool bad = false;
+                u16x2 bad = {0, 0};
 #pragma unroll
                 for (int k = 0; k < S::TileBytes / 16 / kPromptThreads; ++k) {
                     const int i = tid + k * kPromptThreads;
-                    half8v *y = (half8v *)(values + 16 * i);
-                    if (u * S::Tokens + i / (D / 8) >= end) *y = half8v{};
-                    else bad |= any_not_finite(*y);
+                    U4 *y = (U4 *)(values + 16 * i);
+                    if (u * S::Tokens + i / (D / 8) >= end) *y = U4{0, 0, 0, 0};
+                    else bad = most_magnitude(bad, *y);
                 }
-                if (__syncthreads_or(bad)) {
+                if (__ballot(bad[0] >= 0x7c00 || bad[1] >= 0x7c00) && lane == 0) s_bad = u + 1;
+                __syncthreads();
+                if (__builtin_amdgcn_readfirstlane(s_bad) == u + 1) {
                     for (int i = 32 * NB * wn; i < 32 * NB * (wn + 1); ++i) {
                         const bool seen = u * S::Tokens + i >= lo && u * S::Tokens + i < hi;
 #pragma unroll

@@ -73,7 +73,8 @@ def attention(q, k, v, scale, lo, hi, p, cap=0.0, slopes=None, rounded=True):
         score = (D + 4) * 2.0 ** -24 * (np.abs(kk) @ np.abs(qq)) * abs(scale)
         if cap:
             x = cap * np.tanh(x / cap)
-            score = score + 2.0 ** -21 * np.abs(x)           # 2^-22 of tanh, and the factor
+            # 2^-22 of tanh, and the factor; (1 - e) / (1 + e) of an e that is off by 2^-23 of itself: half of that where e is 1
+            score = score + 2.0 ** -21 * np.abs(x) + (2.0 ** -24 * cap if cap <= 64 else 0)
         if slopes is not None:
             x = x - float(slopes[h]) * away
             score = score + 2.0 ** -22 * float(abs(slopes[h])) * away
