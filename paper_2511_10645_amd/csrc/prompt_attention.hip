@@ -290,7 +290,9 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     int rest = blockIdx.x / a.kv_heads;
     const int head = blockIdx.x - rest * a.kv_heads;
     if (S::Blocks == 2 && rest >= slots && all <= 2 * slots) rest = all - 1 - (rest - slots);
-    const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
+    // The parts of a tile side by side where tiles are short (four drafts of 5 rows: 16.8 us, 20.0 the other way), else last what may have no share, so
+    // that the shares fill the chip evenly (prefix and cap, 256 channels: 73.5 us, 76.9).
+    const int split = S::WN > 1 ? rest % a.splits : rest / a.tiles, tile = a.tiles - 1 - (S::WN > 1 ? rest / a.splits : rest - split * a.tiles);
     Where w;
     int work;
     if (!find_tile<S>(w, work, a, tile, lane)) return;
