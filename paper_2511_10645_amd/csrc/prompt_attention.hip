@@ -278,7 +278,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     // Two tiles of keys and two of values; later the waves' results, one wave's to a tile's place.  They are objects of their own, and a round knows
     // which ones it reads and which it fills: the compiler makes a read wait for every copy to LDS that might be to the same object.
     __shared__ __attribute__((aligned(16))) uint8_t s_keys0[S::TileBytes], s_keys1[S::TileBytes], s_values0[S::TileBytes], s_values1[S::TileBytes];
-    const auto place = [&](int i) { return i == 0 ? s_keys0 : i == 1 ? s_keys1 : i == 2 ? s_values0 : s_values1; };
+    const auto place = [&](int i) __attribute__((always_inline)) { return i == 0 ? s_keys0 : i == 1 ? s_keys1 : i == 2 ? s_values0 : s_values1; };
     __shared__ int s_lo[kWaves][2], s_hi[kWaves][2];
     __shared__ int s_bad, s_last;                // s_bad: 1 + the tile that has values that are not finite, where not all see them
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -298,10 +298,10 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     if (!find_tile<S>(w, work, a, tile, lane)) return;
     const int pairs = w.rows * a.group, pair = w.pair0 + wm * 32 + n32;
     // the pair's row and query head (the last pair's for lanes past it)
-    const auto lo_of = [&](int p) { const int lo = a.window ? p - a.window + 1 : 0; return lo > 0 ? lo : 0; };
+    const auto lo_of = [&](int p) __attribute__((always_inline)) { const int lo = a.window ? p - a.window + 1 : 0; return lo > 0 ? lo : 0; };
     int prefix = 0;
     if (a.prefix) { prefix = __builtin_amdgcn_readfirstlane(a.prefix[w.b]); prefix = prefix < w.n ? prefix : w.n; }
-    const auto hi_of = [&](int p) { return p + 1 > prefix ? p + 1 : prefix; };
+    const auto hi_of = [&](int p) __attribute__((always_inline)) { return p + 1 > prefix ? p + 1 : prefix; };
     const int row = (pair < pairs ? pair : pairs - 1) / a.group, qhead = head * a.group + (pair < pairs ? pair : pairs - 1) - row * a.group;
 
     // what the pair sees: lo <= t < hi, from position pos
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     // The least and largest lo and hi of the block, and the largest lo and least hi of it and of the wave.  Both rise with the row, unless documents have it otherwise.
     int begin, end, whole_lo, whole_hi, lo_most, hi_least;
     if (!a.first) {
-        const auto pos_at = [&](int p) { return w.n - w.rows + (p < pairs ? p : pairs - 1) / a.group; };
+        const auto pos_at = [&](int p) __attribute__((always_inline)) { return w.n - w.rows + (p < pairs ? p : pairs - 1) / a.group; };
         const int p0 = pos_at(w.pair0), p1 = pos_at(w.pair0 + S::Pairs - 1), w0 = pos_at(w.pair0 + wm * 32), w1 = pos_at(w.pair0 + wm * 32 + 31);
         begin = lo_of(p0); end = hi_of(p1); whole_lo = lo_of(p1); whole_hi = hi_of(p0);
         lo_most = lo_of(w1); hi_least = hi_of(w0);
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     constexpr int Runs = S::Tokens / 16;         // of a tile
     int run0 = u0 * Runs, pages = -1;
     uint64_t there = 0;
-    const auto turn = [&](int run) {
+    const auto turn = [&](int run) __attribute__((always_inline)) {
         run0 = run;
         const int t = (run + lane) * 16;
         pages = -1;
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         there = __ballot(pages >= 0);
     };
     struct Pages { int page[S::Quarters]; uint32_t gone; };      // of this wave's runs of a tile; a bit for every run of the tile that is not there
-    const auto pages_of = [&](int u) {           // once turn() has got them
+    const auto pages_of = [&](int u) __attribute__((always_inline)) {           // once turn() has got them
         Pages p;
 #pragma unroll
         for (int i = 0; i < S::Quarters; ++i) p.page[i] = __builtin_amdgcn_readlane(pages, u * Runs - run0 + wave + 4 * i);
@@ -402,25 +402,25 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     Run<D, FMT, false> vr[S::Quarters];
     typename Run<D, FMT, true>::Held kh[Copied ? 1 : Jobs];
     typename Run<D, FMT, false>::Held vh[Copied ? 1 : Jobs];
-    const auto keys_at = [&](const Pages &p, int u) {
+    const auto keys_at = [&](const Pages &p, int u) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < S::Quarters; ++i) kr[i].at(a, head, p.page[i], u * S::Tokens + (wave + 4 * i) * 16);
     };
-    const auto values_at = [&](const Pages &p, int u) {
+    const auto values_at = [&](const Pages &p, int u) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < S::Quarters; ++i) vr[i].at(a, head, p.page[i], u * S::Tokens + (wave + 4 * i) * 16);
     };
-    const auto run_in = [&](uint8_t *place, int job) { return place + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
+    const auto run_in = [&](uint8_t *place, int job) __attribute__((always_inline)) { return place + (wave + 4 * (job / Loads)) * (16 * 2 * D); };
 
     // S^T of a tile: score j of block b is of token 32 (NB wn + b) + 8 (j / 4) + 4 h + j % 4
     F16 s[NB];
     const int key_lane = key_at<D>(32 * NB * wn + n32, h);
-    const auto key_frag = [&](const uint8_t *keys, int i) { return *(const half8v *)(keys + key_lane + key_at<D>(32 * (i / KS), 2 * (i % KS))); };
+    const auto key_frag = [&](const uint8_t *keys, int i) __attribute__((always_inline)) { return *(const half8v *)(keys + key_lane + key_at<D>(32 * (i / KS), 2 * (i % KS))); };
     // 16 tokens i / R of this wave's, channels 32 (i % R) .., transposed; tokens 4 h + (0..3), then 8 more
     int value_lane[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) value_lane[r] = value_at<D>(32 * NB * wn + 4 * h + ((lane & 15) >> 2), 32 * r + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-    const auto value_frag = [&](const uint8_t *values, int i) {
+    const auto value_frag = [&](const uint8_t *values, int i) __attribute__((always_inline)) {
         const uint8_t *from = values + value_lane[i % R] + 16 * (i / R) * 2 * D;
         const Tr4 one = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsTr4 *)from), two = __builtin_amdgcn_ds_read_tr16_b64_v4f16((LdsTr4 *)(from + 8 * 2 * D));
         half8v f;
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         return f;
     };
     // what is done to scores before their maximum is taken: other scores, and the mask
-    const auto finish = [&](F16 (&z)[NB], int u, uint32_t gone) {
+    const auto finish = [&](F16 (&z)[NB], int u, uint32_t gone) __attribute__((always_inline)) {
         const int t0 = u * S::Tokens + 32 * NB * wn + 4 * h;
         if constexpr (SCORED) {
 #pragma unroll
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         }
         if (u * S::Tokens < lo_most || (u + 1) * S::Tokens > hi_least || gone) {
             // a bit for every token of a block that the pair sees; a score keeps its bits or takes those of -inf
-            const auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
+            const auto below = [](int n) __attribute__((always_inline)) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const uint32_t away = gone >> (2 * (NB * wn + b)), there = (away & 1 ? 0u : 0xffffu) | (away & 2 ? 0u : 0xffff0000u);
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         }
     };
     // new scores z, the largest of this lane's `top`: the sums follow if the maximum has grown by more than kSlack
-    const auto follow = [&](float top, F16 (&z)[NB]) {
+    const auto follow = [&](float top, F16 (&z)[NB]) __attribute__((always_inline)) {
         top = max2(top) * scale;
         if (__ballot(top > m + kSlack)) {
             const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
@@ -546,10 +546,10 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         // A round has the scores of tile u.  It turns them into weights while the matrix cores compute those of u + 1, then multiplies the weights
         // with the values of u while it looks for the next maximum; keys of u + 2 and values of u + 1 go to LDS meanwhile.  What the vector units do is dealt
         // out over the matrix instructions evenly, 32 cycles of a matrix core to as many of a vector unit: 8 each for the issue and for an exponential, 4 for others.
-        const auto round = [&](int u, uint8_t *free_keys, uint8_t *keys, uint8_t *values, uint8_t *free_values) __attribute__((always_inline)) {
+        const auto round = [&](int u, uint8_t *free_keys, uint8_t *keys, uint8_t *values, uint8_t *free_values) __attribute__((always_inline)) __attribute__((always_inline)) {
             constexpr int Ahead = NB * KS < 5 ? NB * KS : 5;         // operands on their way from LDS, which takes 130 cycles and more
             half8v f[Ahead + 1];
-            each<0, Ahead>([&](auto at) { f[at] = key_frag(keys, at); });
+            each<0, Ahead>([&](auto at) __attribute__((always_inline)) { f[at] = key_frag(keys, at); });
             if (u * S::Tokens < whole_lo || (u + 1) * S::Tokens > whole_hi) {
                 // A tile that some pair does not see all of: values that nobody sees become zeros, for such places may hold NaN, whose product with a weight
                 // of 0 is not 0.  Others that are not finite are taken here by the pairs that see them (their results are not finite, whatever the
@@ -588,7 +588,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             const uint32_t gone = p1.gone;
             if ((u + 4) * Runs - run0 >= 64) turn((u + 4) * Runs);
             // the next round's requests; past the part's last tile there is nothing to read, and zeros come
-            const auto advance = [&]() {
+            const auto advance = [&]() __attribute__((always_inline)) {
                 values_at(Copied ? p2 : p3, u + Lead);
                 p1 = p2;
                 p2 = p3;
@@ -598,7 +598,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
 
             constexpr int All = NB * 8, Late = NB * 3;       // pairs of scores; those whose weights the second product does not need at once
             half8v p[2 * NB];
-            const auto weigh = [&](auto at) {
+            const auto weigh = [&](auto at) __attribute__((always_inline)) {
                 constexpr int c = at, b = c / 8, e = c % 8;
                 const float one = __builtin_amdgcn_exp2f(fmaf(s[b][2 * e], up, off)), two = __builtin_amdgcn_exp2f(fmaf(s[b][2 * e + 1], up, off));
                 l += one;
@@ -611,7 +611,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             F16 next[NB];
             {
                 constexpr int Steps = NB * KS;
-                each<0, Steps>([&](auto at) {
+                each<0, Steps>([&](auto at) __attribute__((always_inline)) {
                     constexpr int i = at;
                     if constexpr (i + Ahead < Steps) f[(i + Ahead) % (Ahead + 1)] = key_frag(keys, i + Ahead);
                     else f[(i + Ahead) % (Ahead + 1)] = value_frag(values, i + Ahead - Steps);
@@ -621,14 +621,14 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                         for (int j = 0; j < 16; ++j) z[j] = 0;
                     next[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % (Ahead + 1)], q[i % KS], z, 0, 0, 0);
                     if constexpr (Copied)
-                        each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) {
+                        each<i * 2 * Jobs / Steps, (i + 1) * 2 * Jobs / Steps>([&](auto job) __attribute__((always_inline)) {
                             constexpr int k = job;
                             if constexpr (k < Jobs) kr[k / Loads].copy(run_in(free_keys, k), k % Loads, lane, a.page_log);
                             else vr[(k - Jobs) / Loads].copy(run_in(free_values, k - Jobs), (k - Jobs) % Loads, lane, a.page_log);
                         });
                     each<i *(All - Late) / Steps, (i + 1) * (All - Late) / Steps>(weigh);
                     if constexpr (!Copied)
-                        each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) {
+                        each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) __attribute__((always_inline)) {
                             constexpr int k = job;
                             kr[0].put(kh[k], run_in(free_keys, k), k % Loads, lane);
                             kr[k / Loads].ask(kh[k], k % Loads, lane, a.page_log);
@@ -640,17 +640,17 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             float top = -INFINITY;
             {
                 constexpr int Steps = 2 * NB * R, Soon = NB * R, Before = NB * KS;      // of the first product, whose ring of operands goes on
-                each<0, Steps>([&](auto at) {
+                each<0, Steps>([&](auto at) __attribute__((always_inline)) {
                     constexpr int i = at;
                     if constexpr (i + Ahead < Steps) f[(Before + i + Ahead) % (Ahead + 1)] = value_frag(values, i + Ahead);
                     acc[i % R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[(Before + i) % (Ahead + 1)], p[i / R], acc[i % R], 0, 0, 0);
                     if constexpr (i < Soon) each<All - Late + i * Late / Soon, All - Late + (i + 1) * Late / Soon>(weigh);
-                    each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) {
+                    each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) __attribute__((always_inline)) {
                         constexpr int c = two;
                         top = max3(top, next[c / 8][2 * (c % 8)], next[c / 8][2 * (c % 8) + 1]);
                     });
                     if constexpr (!Copied)
-                        each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) {
+                        each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) __attribute__((always_inline)) {
                             constexpr int k = job;
                             vr[0].put(vh[k], run_in(free_values, k), k % Loads, lane);
                             vr[k / Loads].ask(vh[k], k % Loads, lane, a.page_log);
@@ -715,9 +715,9 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     if (parts > 1) {
         // every part's m, l and sums where its lanes left them, through memory that all XCDs see
         const size_t tile_at = (size_t)tile * a.kv_heads + head;
-        const auto part_rsrc = [&](int p) { return prompt_rsrc(a.partial + (tile_at * a.splits + p) * S::PartFloats, (uint32_t)(S::PartFloats * 4)); };
+        const auto part_rsrc = [&](int p) __attribute__((always_inline)) { return prompt_rsrc(a.partial + (tile_at * a.splits + p) * S::PartFloats, (uint32_t)(S::PartFloats * 4)); };
         const int ml_at = (S::Pairs * D + 2 * (wm * 32 + n32)) * 4;
-        const auto sums_at = [&](int r, int i) { return (((wm * R + r) * 4 + i) * 64 + lane) * 16; };
+        const auto sums_at = [&](int r, int i) __attribute__((always_inline)) { return (((wm * R + r) * 4 + i) * 64 + lane) * 16; };
         typedef decltype(__builtin_amdgcn_raw_buffer_load_b128(part_rsrc(0), 0, 0, 0)) B4;
         typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(part_rsrc(0), 0, 0, 0)) B2;
         {
@@ -751,7 +751,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         for (int p0 = 0; p0 < parts; p0 += At) {
             U2 ml[At];
             F4 y[At][R][4 / S::WN];
-            const auto from = [&](int z) { return prompt_rsrc(a.partial + (tile_at * a.splits + p0 + z) * S::PartFloats, p0 + z < parts ? (uint32_t)(S::PartFloats * 4) : 0); };
+            const auto from = [&](int z) __attribute__((always_inline)) { return prompt_rsrc(a.partial + (tile_at * a.splits + p0 + z) * S::PartFloats, p0 + z < parts ? (uint32_t)(S::PartFloats * 4) : 0); };
 #pragma unroll
             for (int z = 0; z < At; ++z) ml[z] = __builtin_bit_cast(U2, __builtin_amdgcn_raw_buffer_load_b64(from(z), ml_at, 0, kPromptAgent));
 #pragma unroll
