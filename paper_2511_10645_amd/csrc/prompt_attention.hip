@@ -720,7 +720,8 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         const auto sums_at = [&](int r, int i) __attribute__((always_inline)) { return (((wm * R + r) * 4 + i) * 64 + lane) * 16; };
         typedef decltype(__builtin_amdgcn_raw_buffer_load_b128(part_rsrc(0), 0, 0, 0)) B4;
         typedef decltype(__builtin_amdgcn_raw_buffer_load_b64(part_rsrc(0), 0, 0, 0)) B2;
-        {
+        const bool live = w.pair0 + wm * 32 < pairs;         // a wave without pairs has nothing to leave and nothing to join
+        if (live) {
             const __amdgpu_buffer_rsrc_t to = part_rsrc(split);
             if (h == 0 && wn == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(B2, U2{__float_as_uint(m), __float_as_uint(l)}), to, ml_at, 0, kPromptAgent);
 #pragma unroll
@@ -748,7 +749,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[r][j] = 0;
-        for (int p0 = 0; p0 < parts; p0 += At) {
+        for (int p0 = 0; p0 < (live ? parts : 0); p0 += At) {
             U2 ml[At];
             F4 y[At][R][4 / S::WN];
             const auto from = [&](int z) __attribute__((always_inline)) { return prompt_rsrc(a.partial + (tile_at * a.splits + p0 + z) * S::PartFloats, p0 + z < parts ? (uint32_t)(S::PartFloats * 4) : 0); };
@@ -828,7 +829,7 @@ static int64_t prompt_splits(int64_t tiles, int64_t kv_heads)
 // The shapes that calls choose from, by what they have of pairs.
 template <int D> struct Shapes;
 template <> struct Shapes<64> { typedef Shape<64, 2, 1> Many; typedef Shape<64, 1, 4> Few; };
-template <> struct Shapes<128> { typedef Shape<128, 2, 1> Many; typedef Shape<128, 1, 4> Few; };
+template <> struct Shapes<128> { typedef Shape<128, 2, 1> Many; typedef Shape<128, 1, 2> Few; };
 template <> struct Shapes<256> { typedef Shape<256, 2, 1> Many; typedef Shape<256, 1, 2> Few; };
 constexpr int kFewPairs = 64;                    // of a sequence on average, up to which
 
