@@ -1,10 +1,10 @@
 """One quantised decoder layer that serves tokens: prompts into a paged cache, then one token of every sequence after the other.
 
-    python examples/decode_layer.py [--batch 16] [--prompt 512] [--steps 64] [--cache fp16|e4m3] [--tiny]
+    python examples/decode_layer.py [--batch 16] [--prompt 512] [--steps 64] [--cache fp16|e4m3|mxfp4] [--tiny]
 
 The linears are the library's rotated W4A16 ones (random weights, transformed and quantised here), and everything between
 them is the library's too, but for the gate's activation, which is torch's: norm with the residual, rotary positions on the way into the cache,
-attention over the cache.  The decode step is captured once as a HIP graph and replayed.
+attention over the cache, of whole prompts and of single tokens.  The decode step is captured once as a HIP graph and replayed.
 """
 from __future__ import annotations
 
@@ -57,17 +57,22 @@ class DecoderLayer:
     def workspace(self, tokens):
         """One for all calls of any of these token counts."""
         linears = (self.qkv, self.o, self.gate_up, self.down)
-        return paro.Workspace.shared([(x.rot, x.w, t) for x in linears for t in tokens], attention=[(self.cache, self.q_heads, t) for t in tokens])
+        return paro.Workspace.shared([(x.rot, x.w, t) for x in linears for t in tokens], attention=[(self.cache, self.q_heads, t) for t in tokens],
+                                     prompts=[(self.cache, self.q_heads, t, t) for t in tokens])
 
-    def __call__(self, x, residual, positions, slots, table, lengths, ws):
-        """x [T][hidden], one row per token; table and lengths: the tokens that each row attends to, its own among them."""
+    def __call__(self, x, residual, positions, slots, table, lengths, ws, starts=None):
+        """x [T][hidden], one row per token; table and lengths: of the sequences, the rows' own tokens among them.  A row is a sequence's newest token, or,
+        with starts, rows starts[b] .. starts[b+1] - 1 are sequence b's newest ones."""
         if residual is None:
             n, h = paro.paro_rms_norm(x, self.norms[0], EPS), x
         else:
             n, h = paro.paro_rms_norm(x, self.norms[0], EPS, residual=residual)
         q, k, v = self.qkv(n, ws).split((self.q, self.kv, self.kv), 1)
         q = paro.paro_kv_append(self.cache, k, v, slots, self.rope, positions, q, q)
-        a = paro.paro_paged_attention(self.cache, q, table, lengths, ws)
+        if starts is None:
+            a = paro.paro_paged_attention(self.cache, q, table, lengths, ws)
+        else:
+            a = paro.paro_prompt_attention(self.cache, q, starts, table, lengths, ws)
         n, h = paro.paro_rms_norm(self.o(a, ws), self.norms[1], EPS, residual=h)
         gate, up = self.gate_up(n, ws).split((self.mlp, self.mlp), 1)
         return self.down(torch.nn.functional.silu(gate) * up, ws), h
@@ -89,12 +94,13 @@ class Sequences:
 
 
 def prefill(layer: DecoderLayer, seqs: Sequences, x, ws):
-    """x [batch][tokens][hidden]: the same number of prompt tokens for every sequence.  Every token is a row of its own that
-    attends to the tokens before it; keys and values of all are in the cache before the attention reads it."""
+    """x [batch][tokens][hidden]: the same number of prompt tokens for every sequence.  Keys and values of all are in the cache before the
+    attention reads it."""
     b, t, hidden = x.shape
     sequence = torch.arange(b, device="cuda").repeat_interleave(t)
     positions = (seqs.lengths[:, None] + torch.arange(t, device="cuda", dtype=torch.int32)).flatten()
-    y, h = layer(x.reshape(b * t, hidden), None, positions, seqs.slots(sequence, positions), seqs.table[sequence], positions + 1, ws)
+    starts = torch.arange(b + 1, device="cuda", dtype=torch.int32) * t
+    y, h = layer(x.reshape(b * t, hidden), None, positions, seqs.slots(sequence, positions), seqs.table, seqs.lengths + t, ws, starts)
     seqs.lengths += t
     return (y + h).view(b, t, hidden)
 
@@ -139,7 +145,7 @@ def main():
     ap.add_argument("--batch", type=int, default=16)
     ap.add_argument("--prompt", type=int, default=512)
     ap.add_argument("--steps", type=int, default=64)
-    ap.add_argument("--cache", choices=("fp16", "e4m3"), default="fp16")
+    ap.add_argument("--cache", choices=("fp16", "e4m3", "mxfp4"), default="fp16")
     ap.add_argument("--tiny", action="store_true")
     a = ap.parse_args()
     shape = SHAPES["tiny" if a.tiny else "8b"]

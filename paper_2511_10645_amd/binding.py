@@ -254,6 +254,7 @@ class _CtypesCalls:
         ldq, B = _gpu_rows(Q), Q.shape[0]
         heads = _attention_inputs(cache, Q, table, lengths, buf, window, B)
         scores = _scores(cap, slopes, heads, Q)
+        _current(Q)
         O, ldo = _rows_or_new(O, B, Q.shape[1], Q)
         lse = torch.empty((B, heads), dtype=torch.float32, device=Q.device) if with_lse else None
         st = lib().paro_paged_attention_scored(ctypes.byref(cache), Q.data_ptr(), ldq, heads, table.data_ptr(), table.shape[1] if B == 1 else table.stride(0),
@@ -271,6 +272,7 @@ class _CtypesCalls:
         if first is not None:
             _gpu_vector(first, torch.int32, T, Q)
         scores = _scores(cap, slopes, heads, Q)
+        _current(Q)
         O, ldo = _rows_or_new(O, T, Q.shape[1], Q)
         lse = torch.empty((T, heads), dtype=torch.float32, device=Q.device) if with_lse else None
         st = lib().paro_prompt_attention(ctypes.byref(cache), Q.data_ptr(), ldq, heads, T, starts.data_ptr(), table.data_ptr(),
@@ -568,7 +570,6 @@ def _attention_inputs(cache, Q, table, lengths, buf, window: int, B: int) -> int
     assert table.is_cuda and buf.is_cuda, "expected a tensor on the GPU"
     for device in (table.device.index, buf.device.index, cache.device):
         _same_gpu(device, Q)
-    _current(Q)
     assert table.shape[1] < 2 ** 31 and B < 2 ** 31
     _number(window)
     return Q.shape[1] // cache.head_dim

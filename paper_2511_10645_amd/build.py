@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libparo.so")
 HOST_LIB = os.path.join(HERE, "paro_host.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
-SOURCES = ["paro_api.hip", "rotate.hip", "w4_layout.hip", "decode.hip", "decode_wide.hip", "gemm.hip", "linear_rows.hip", "linear_ic.hip", "linear_tile.hip", "quantize.hip", "quantize_weight.hip", "ceilings.hip", "fwht.hip", "mxfp4.hip", "norm.hip", "rope.hip", "paged_attention.hip", "prompt_attention.hip"]
+SOURCES = ["paro_api.hip", "rotate.hip", "w4_layout.hip", "decode.hip", "decode_wide.hip", "gemm.hip", "linear_rows.hip", "linear_ic.hip", "linear_tile.hip", "quantize.hip", "quantize_weight.hip", "ceilings.hip", "fwht.hip", "mxfp4.hip", "norm.hip", "rope.hip", "paged_attention.hip", "prompt_attention.hip", "prompt_fp16.hip", "prompt_e4m3.hip", "prompt_mxfp4.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -337,7 +337,7 @@ struct Attention {
     int32_t window;
     paro_scores_t scores;
 
-    // false with an exception set; batch < 0: as many sequences as rows
+    // false with an exception set.  Whether their GPU is the current one is asked last, once a call's other tensors are known to be there too.
     bool take(PyObject *cache, PyObject *Q, PyObject *block_table, PyObject *lens, PyObject *workspace, PyObject *nbytes, PyObject *scale_, PyObject *window_,
               PyObject *cap, PyObject *slopes_, bool row_each)
     {
@@ -352,7 +352,7 @@ struct Attention {
         if (table->scalar_type() != at::kInt || table->dim() != 2 || (table->stride(1) != 1 && table->size(1) != 1) || (row_each && table->size(0) != q->size(0)))
             return refuse("expected a block table of int32 rows, one per sequence");
         batch = table->size(0);
-        if (!on_gpu(*table, *q) || !gpu_vector(*lengths, at::kInt, batch, *q) || !on_gpu(*ws, *q) || !same_gpu(held->device, *q) || !current(*q)) return false;
+        if (!on_gpu(*table, *q) || !gpu_vector(*lengths, at::kInt, batch, *q) || !on_gpu(*ws, *q) || !same_gpu(held->device, *q)) return false;
         bytes = PyLong_AsSize_t(nbytes);
         scale = (float)PyFloat_AsDouble(scale_);
         if (PyErr_Occurred() || !number(window_, window)) return false;
@@ -375,7 +375,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     HANDLE_TH_ERRORS
     if (n != 10 && n != 12) { PyErr_SetString(PyExc_TypeError, "paged_attention takes 10 or 12 arguments"); return nullptr; }
     Attention x;
-    if (!x.take(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], n == 12 ? a[10] : nullptr, n == 12 ? a[11] : nullptr, true)) return nullptr;
+    if (!x.take(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], n == 12 ? a[10] : nullptr, n == 12 ? a[11] : nullptr, true) || !current(*x.q)) return nullptr;
     const int want = PyObject_IsTrue(a[9]);
     if (want < 0) return nullptr;
     at::Tensor o = rows_or_new(a[8], x.batch, x.q->size(1), *x.q), lse;
@@ -406,7 +406,7 @@ PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor *starts = tensor(a[2]), *prefix, *first;
     if (!starts || !maybe(a[11], prefix) || !maybe(a[12], first)) return nullptr;
     if (!gpu_vector(*starts, at::kInt, x.batch + 1, *x.q) || (prefix && !gpu_vector(*prefix, at::kInt, x.batch, *x.q)) ||
-        (first && !gpu_vector(*first, at::kInt, T, *x.q)))
+        (first && !gpu_vector(*first, at::kInt, T, *x.q)) || !current(*x.q))
         return nullptr;
     const int want = PyObject_IsTrue(a[14]);
     if (want < 0) return nullptr;
