@@ -464,8 +464,8 @@ class Workspace:
     @classmethod
     def shared(cls, calls, device="cuda", attention=(), prompts=()):
         """One workspace for calls of several shapes: calls = [(rot or None, weight, T), ...], attention = [(cache, q_heads,
-        batch), ...], prompts = [(cache, q_heads, T, batch), ...] (which serves fewer rows and sequences too).  Sized as the largest exchange part plus the largest scratch part, so no call's scratch touches
-        another's exchange part."""
+        batch), ...], prompts = [(cache, q_heads, T, batch), ...] (which serves fewer rows and sequences too).  Sized as the largest
+        exchange part plus the largest scratch part, so no call's scratch touches another's exchange part."""
         ex = sc = 0
         for rot, w, T in calls:
             total, e = paro_workspace_bytes(rot, w, T), paro_workspace_exchange_bytes(rot, w, T)
