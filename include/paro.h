@@ -475,11 +475,12 @@ paro_status paro_paged_attention_scored(const paro_kv_cache *cache, const paro_h
  * prefix: device [batch], tokens of the sequence's begin that its rows see from both sides (at most n count), or NULL; first: device [T], the first token
  * of each row's document, where several lie in one sequence, or NULL.
  * Otherwise as paro_paged_attention_scored, with one row of O (and of lse, fp32 [T][q_heads]) per row of Q: cache formats, block table, missing pages,
- * rows with nothing to attend to (also those at p < 0), scores, scale.  A value that is not finite makes its channel's results not finite
+ * rows with nothing to attend to (those at p < 0 have the prefix alone), scores, scale.  A value that is not finite makes its channel's results not finite
  * for the rows that attend to its token, whatever the weight, and for no others.  Weights of the softmax are rounded to fp16 (2^-11) for the product with
  * the values, which paro_paged_attention does not.
  * starts: device [batch + 1], from 0 to T and not falling (rows outside them are left as they were; values out of range are taken as 0 or T, and rows that two
- * sequences claim hold either's results).  T at most 2^24, T * q_heads at most 2^30, table_width * page at most 2^30.  O nowhere in Q.
+ * sequences claim hold either's results).  T at most 2^24, q_heads at most 65535, T * q_heads + 32 kv_heads * min(batch, T) at most
+ * 2^28 (a little beyond it as tiles of rows fall), table_width * page at most 2^30; otherwise PARO_ERR_UNSUPPORTED.  O nowhere in Q.
  * ws: >= paro_workspace_bytes_prompt() bytes, 256-byte aligned, in the two parts described at paro_workspace_bytes(); as with
  * paro_paged_attention, counters in the exchange part are zero again after every call, and blocks never wait for each other. */
 size_t paro_workspace_exchange_bytes_prompt(const paro_kv_cache *cache, int32_t q_heads, int32_t T, int32_t batch);

@@ -51,7 +51,7 @@ extern "C" paro_status paro_prompt_attention(const paro_kv_cache *cache, const p
     const int64_t tokens = (int64_t)table_width * c.page;
     if (q_heads > 65535 || tokens > (int64_t)1 << 30 || T > 1 << 24 || (int64_t)T * q_heads > (int64_t)1 << 30) return PARO_ERR_UNSUPPORTED;
     const int64_t tiles = prompt_tiles(T, q_heads / c.kv_heads, batch, kLeastPairs);
-    if (tiles * c.kv_heads > (int64_t)1 << 23) return PARO_ERR_UNSUPPORTED;       // a launch holds fewer than 2^32 threads
+    if (tiles * c.kv_heads > (int64_t)1 << 23) return PARO_ERR_UNSUPPORTED;       // a launch holds fewer than 2^32 threads: T q_heads + 32 kv_heads min(batch, T) <= 2^28 do
     if (!ws || ws_bytes < paro_workspace_bytes_prompt(cache, q_heads, T, batch)) return PARO_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return PARO_ERR_ALIGN;
 

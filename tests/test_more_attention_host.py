@@ -64,6 +64,16 @@ def test_prompt_refusals():
     assert f(c=_cache(format=4)) == E_NULL and f(c=_cache(page=8)) == E_UNSUP
 
 
+
+@pytest.mark.parametrize("T,batch,hq,hkv,taken", [(2 ** 23 - 64, 1, 32, 8, True), (2 ** 22, 2 ** 17, 32, 8, True), (2 ** 23, 64, 32, 8, False), (2 ** 24, 1, 32, 8, False),
+                                                   (2 ** 24, 1, 15, 5, True), (2 ** 24, 1, 17, 1, False), (64, 2 ** 19, 8, 8, True), (2 ** 22, 2 ** 22, 4, 4, False)])
+def test_prompt_sizes(T, batch, hq, hkv, taken):
+    """T q_heads + 32 kv_heads min(batch, T) up to 2^28 passes every check but the workspace's."""
+    assert taken == (T * hq + 32 * min(batch, T) * hkv <= 2 ** 28)
+    st = paro.lib().paro_prompt_attention(r(_cache(kv_heads=hkv)), FAKE, 65536, hq, T, FAKE, FAKE, 4, 4, FAKE, batch, 0.1, 0, None, None, None, FAKE * 4, 65536, None, None, 0, None)
+    assert st == (E_WS if taken else E_UNSUP)
+
+
 def test_prompt_workspace_serves_smaller_calls():
     L = paro.lib()
     size = lambda T, b, hq=32, **kw: (L.paro_workspace_exchange_bytes_prompt(r(_cache(kv_heads=8, **kw)), hq, T, b), L.paro_workspace_bytes_prompt(r(_cache(kv_heads=8, **kw)), hq, T, b))
