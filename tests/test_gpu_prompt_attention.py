@@ -346,3 +346,15 @@ def test_graphs_streams_and_bindings(P):
     finally:
         B_._host = native
     assert all(torch.equal(a, b) for a, b in zip(step(), one))
+
+
+@pytest.mark.parametrize("fmt", ["fp16", "mxfp4"])
+@pytest.mark.parametrize("D,hq,hkv", [(64, 4, 2), (128, 4, 2), (256, 3, 1)])
+@pytest.mark.parametrize("new,lengths", [([90, 70, 3, 150], [40, 1, 0, 100]), ([9, 3, 5, 1], [4, 1, 0, 1])])
+def test_more_rows_than_tokens(P, fmt, D, hq, hkv, new, lengths):
+    """Rows at positions below 0 see the prefix alone, their distances counted from there; without one, nothing."""
+    say(f"more rows than tokens: {fmt} D {D} new {new} lengths {lengths}")
+    case = filled(P, lengths, hkv, D, 16, fmt, 5)
+    for prefix in (None, [3, 1, 2, 50], [2 ** 31 - 1, -4, 7, 0]):
+        check(P, *case, new, lengths, hq, 7, prefix=prefix)
+        check(P, *case, new, lengths, hq, 8, prefix=prefix, cap=20.0, slopes=slopes_of(hq), window=6)
