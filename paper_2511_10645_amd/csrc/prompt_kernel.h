@@ -513,7 +513,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         // A round has the scores of tile u.  It turns them into weights while the matrix cores compute those of u + 1, then multiplies the weights
         // with the values of u while it looks for the next maximum; keys of u + 2 and values of u + 1 go to LDS meanwhile.  What the vector units do is dealt
         // out over the matrix instructions evenly, 32 cycles of a matrix core to as many of a vector unit: 8 each for the issue and for an exponential, 4 for others.
-        const auto round = [&](int u, uint8_t *free_keys, uint8_t *keys, uint8_t *values, uint8_t *free_values) __attribute__((always_inline)) __attribute__((always_inline)) {
+        const auto round = [&](int u, uint8_t *free_keys, uint8_t *keys, uint8_t *values, uint8_t *free_values) __attribute__((always_inline)) {
             // operands on their way from LDS, which takes 130 cycles and more; fewer where registers are short (prefix and cap, 256 channels: 72.2 us, 73.4 with 5)
             constexpr int Ahead = SCORED ? 3 : NB * KS < 5 ? NB * KS : 5;
             half8v f[Ahead + 1];
