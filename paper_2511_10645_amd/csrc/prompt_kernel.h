@@ -50,12 +50,28 @@ __device__ inline int prompt_sums_upto(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);        // row_bcast 31 into rows 2 and 3
     return x;
 }
-// The largest of three, without the quieting of signalling NaN that fmaxf brings along (an instruction for every value).
+// The largest of three, without the quieting of signalling NaN that fmaxf brings along (an instruction for every value).  The compiler keeps 12 states
+// between a product and the first vector instruction that takes its result, but not in front of inline assembly, whose operands it does not look at:
+// a product's result goes through largest(), which takes its first pair by fmaxf and the others behind it.
 __device__ inline float max3(float a, float b, float c)
 {
     float m;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
     return m;
+}
+// `top` and pair c of a product's result; pairs are taken from the first one on.
+template <int c>
+__device__ __forceinline__ float largest(float top, const F16 &z)
+{
+    if constexpr (c == 0) return fmaxf(top, fmaxf(z[0], z[1]));
+    else return max3(top, z[2 * c], z[2 * c + 1]);
+}
+// The 12 states, where a branch lies between: there the compiler may count along the longer one of two paths that meet.
+__device__ __forceinline__ void product_done()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 11");
+    __builtin_amdgcn_sched_barrier(0);
 }
 // Over the lanes n and n ^ 32, which hold one pair.
 __device__ inline float max2(float x)
@@ -502,12 +518,10 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 for (int j = 0; j < 16; ++j) s[b][j] = 0;
 #pragma unroll
             for (int i = 0; i < NB * KS; ++i) s[i / KS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_frag(keys, i), q[i % KS], s[i / KS], 0, 0, 0);
+            product_done();
             finish(s, u0, p0.gone);
             float top = -INFINITY;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int j = 0; j < 16; j += 2) top = max3(top, s[b][j], s[b][j + 1]);
+            each<0, NB * 8>([&](auto two) __attribute__((always_inline)) { top = largest<two % 8>(top, s[two / 8]); });
             follow(top, s);
         }
         // A round has the scores of tile u.  It turns them into weights while the matrix cores compute those of u + 1, then multiplies the weights
@@ -604,6 +618,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
+            if constexpr (NB == 1) product_done();       // with NB of 2 the next products to be issued lie between
             finish(next, u + 1, gone);
             float top = -INFINITY;
             {
@@ -615,7 +630,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                     if constexpr (i < Soon) each<All - Late + i * Late / Soon, All - Late + (i + 1) * Late / Soon>(weigh);
                     each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) __attribute__((always_inline)) {
                         constexpr int c = two;
-                        top = max3(top, next[c / 8][2 * (c % 8)], next[c / 8][2 * (c % 8) + 1]);
+                        top = largest<c % 8>(top, next[c / 8]);
                     });
                     if constexpr (!Copied)
                         each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) __attribute__((always_inline)) {
