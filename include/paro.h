@@ -476,8 +476,9 @@ paro_status paro_paged_attention_scored(const paro_kv_cache *cache, const paro_h
  * of each row's document, where several lie in one sequence, or NULL.
  * Otherwise as paro_paged_attention_scored, with one row of O (and of lse, fp32 [T][q_heads]) per row of Q: cache formats, block table, missing pages,
  * rows with nothing to attend to (those at p < 0 have the prefix alone), scores, scale.  A value that is not finite makes its channel's results not finite
- * for the rows that attend to its token, whatever the weight, and for no others.  Weights of the softmax are rounded to fp16 (2^-11) for the product with
- * the values, which paro_paged_attention does not.
+ * for the rows that attend to its token, whatever the weight, and for no others.  In the product with the values, weights of the softmax are off by 2^-22 of
+ * themselves or 2^-35 of the row's largest; by 2^-11 in calls with neither a cap nor slopes whose heads have 64 or 128 channels and whose sequences have
+ * more than 64 pairs of a row and a query head to a key-value head on average (T * q_heads > 64 kv_heads * batch), where the matrix cores are the bound.
  * starts: device [batch + 1], from 0 to T and not falling (rows outside them are left as they were; values out of range are taken as 0 or T, and rows that two
  * sequences claim hold either's results).  T at most 2^24, q_heads at most 65535, T * q_heads + 32 kv_heads * min(batch, T) at most
  * 2^28 (a little beyond it as tiles of rows fall), table_width * page at most 2^30; otherwise PARO_ERR_UNSUPPORTED.  O nowhere in Q.

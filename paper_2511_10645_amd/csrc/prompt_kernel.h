@@ -13,9 +13,12 @@
 // in the order 4 (lane/32) + (0..3), then 8 more; values are read from LDS transposed in that order.  The cache's order of keys (16-byte units
 // that interleave the tokens) is the first product's operand order: LDS keeps it, and no access has bank conflicts.
 //
-// p enters the second product as fp16 after a factor of 2^kShift (16 bits would otherwise end at 2^-24 of the maximum): each is off by
-// 2^-11 of itself at most, independently, which adds about as much to a result as its own rounding to fp16 (2.9e-4 instead of 2.0e-4 of the 2-norm); a second
-// fp16 number for the rest, as for single tokens, would cost a product of three, and here the matrix cores are the bound.  Sums stay in fp32.
+// p enters the second product as fp16 numbers after a factor of 2^kShift (16 bits would otherwise end at 2^-24 of the maximum): as two, p and
+// what its rounding left, which together are off by 2^-22 of p or by 2^-35 of the largest, where that product is not what the time goes into:
+// blocks for few rows (0 to 6 % over fp16 caches, 6 to 13 % over others), heads of 256 channels (8 to 13 %), scores with a cap or a bias (8 to 14 %).
+// Otherwise as one, off by 2^-11 of itself at most, independently, which adds about as much to a result as its own rounding to fp16 (2.9e-4 of
+// the 2-norm instead of 2.0e-4): a second one costs 512 rows behind 32256 tokens 375 us instead of 280, 8192 rows 725 instead of 534, 2048 rows
+// 65 instead of 53 (E4M3 71 and 58, MXFP4 69 and 58), 8 x 1024 rows of heads of 64 93 instead of 77.  Sums stay in fp32.
 //
 // Few tiles with long sequences: `splits` blocks share a tile's tokens; each leaves fp32 results in the scratch, and the one that arrives
 // last joins all in their order, so that results do not depend on timing.  Nobody waits.
@@ -258,6 +261,7 @@ template <class S, int FMT, bool SCORED>
 __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_kernel(const PromptArgs a)
 {
     constexpr int D = S::D, NB = S::NB, R = D / 32, KS = D / 16;       // channel tiles of the result, steps of the first product
+    constexpr bool Two = S::WN > 1 || D == 256 || SCORED;              // numbers that a weight is, as above
     // Two tiles of keys and two of values; later the waves' results, one wave's to a tile's place.  They are objects of their own, and a round knows
     // which ones it reads and which it fills: the compiler makes a read wait for every copy to LDS that might be to the same object.
     __shared__ __attribute__((aligned(16))) uint8_t s_keys0[S::TileBytes], s_keys1[S::TileBytes], s_values0[S::TileBytes], s_values1[S::TileBytes];
@@ -579,7 +583,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             };
 
             constexpr int All = NB * 8, Late = NB * 3;       // pairs of scores; those whose weights the second product does not need at once
-            half8v p[2 * NB];
+            half8v p[2 * NB], low[2 * NB];
             const auto weigh = [&](auto at) __attribute__((always_inline)) {
                 constexpr int c = at, b = c / 8, e = c % 8;
                 const float one = __builtin_amdgcn_exp2f(fmaf(s[b][2 * e], up, off)), two = __builtin_amdgcn_exp2f(fmaf(s[b][2 * e + 1], up, off));
@@ -589,6 +593,12 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                 asm volatile("" : "+v"(both), "+v"(l));      // here, not where they are needed
                 p[c / 4][2 * (e & 3)] = both[0];
                 p[c / 4][2 * (e & 3) + 1] = both[1];
+                if constexpr (Two) {
+                    half2v more = {(_Float16)(one - (float)both[0]), (_Float16)(two - (float)both[1])};
+                    asm volatile("" : "+v"(more));
+                    low[c / 4][2 * (e & 3)] = more[0];
+                    low[c / 4][2 * (e & 3) + 1] = more[1];
+                }
             };
             F16 next[NB];
             {
@@ -627,6 +637,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                     constexpr int i = at;
                     if constexpr (i + Ahead < Steps) f[(Before + i + Ahead) % (Ahead + 1)] = value_frag(values, i + Ahead);
                     acc[i % R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[(Before + i) % (Ahead + 1)], p[i / R], acc[i % R], 0, 0, 0);
+                    if constexpr (Two) acc[i % R] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[(Before + i) % (Ahead + 1)], low[i / R], acc[i % R], 0, 0, 0);
                     if constexpr (i < Soon) each<All - Late + i * Late / Soon, All - Late + (i + 1) * Late / Soon>(weigh);
                     each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) __attribute__((always_inline)) {
                         constexpr int c = two;
