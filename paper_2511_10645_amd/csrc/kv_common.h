@@ -86,7 +86,12 @@ inline paro_status check_scores(const paro_scores_t *s, float scale, Scores &to)
     if (!s) return PARO_OK;
     if (!(s->cap >= 0.0f) || !std::isfinite(s->cap * kLog2e) || (s->cap > 0.0f && !std::isfinite(scale / s->cap))) return PARO_ERR_SHAPE;
     if (s->slopes && !aligned(s->slopes, 4)) return PARO_ERR_ALIGN;
-    if (s->cap > 0.0f) { to.cap = s->cap * kLog2e; to.per_cap = scale / s->cap; }
+    if (s->cap > 0.0f) {
+        // Kept within 2^125: capped() takes it 2 log2(e) times, and infinity times a score of 0 would be NaN.  Others are 2^-48 and more, as products
+        // of fp16 values are multiples of that, and their tanh is 1 either way.
+        to.cap = s->cap * kLog2e;
+        to.per_cap = std::fmin(std::fmax(scale / s->cap, -0x1p125f), 0x1p125f);
+    }
     to.slopes = s->slopes;
     return PARO_OK;
 }
