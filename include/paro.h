@@ -479,8 +479,8 @@ paro_status paro_paged_attention_scored(const paro_kv_cache *cache, const paro_h
  * for the rows that attend to its token, whatever the weight, and for no others.  In the product with the values, weights of the softmax are off by 2^-22 of
  * themselves or 2^-35 of the row's largest; by 2^-11 in calls with neither a cap nor slopes whose heads have 64 or 128 channels and whose sequences have
  * more than 64 pairs of a row and a query head to a key-value head on average (T * q_heads > 64 kv_heads * batch), where the matrix cores are the bound.
- * starts: device [batch + 1], from 0 to T and not falling (rows outside them are left as they were; values out of range are taken as 0 or T, and rows that two
- * sequences claim hold either's results).  T at most 2^24, q_heads at most 65535, T * q_heads + 32 kv_heads * min(batch, T) at most
+ * starts: device [batch + 1], from 0 to T and not falling (rows outside them are left as they were; a value out of range is taken as 0 or T, one
+ * below another before it as that one).  T at most 2^24, q_heads at most 65535, T * q_heads + 32 kv_heads * min(batch, T) at most
  * 2^28 (a little beyond it as tiles of rows fall), table_width * page at most 2^30; otherwise PARO_ERR_UNSUPPORTED.  O nowhere in Q.
  * ws: >= paro_workspace_bytes_prompt() bytes, 256-byte aligned, in the two parts described at paro_workspace_bytes(); as with
  * paro_paged_attention, counters in the exchange part are zero again after every call, and blocks never wait for each other. */

@@ -53,6 +53,17 @@ __device__ inline int prompt_sums_upto(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);        // row_bcast 31 into rows 2 and 3
     return x;
 }
+// The largest of lanes 0..lane, of numbers from 0 on.
+__device__ inline int prompt_most_upto(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+    return x;
+}
 // The largest of three, without the quieting of signalling NaN that fmaxf brings along (an instruction for every value).  The compiler keeps 12 states
 // between a product and the first vector instruction that takes its result, but not in front of inline assembly, whose operands it does not look at:
 // a product's result goes through largest(), which takes its first pair by fmaxf and the others behind it.
@@ -91,12 +102,12 @@ __device__ inline float sum2(float x)
 // A tile of pairs: of sequence b, whose rows are row0 .. row0 + rows - 1 and whose tokens are 0 .. n - 1; the tile's first pair.
 struct Where { int b, row0, rows, n, pair0; };
 
-// Tile `tile` of all sequences' tiles, and about how many tiles of tokens all of them have; false: there are fewer.  starts are taken as
-// they come, within 0..T and not falling.
+// Tile `tile` of all sequences' tiles, and about how many tiles of tokens all of them have; false: there are fewer.  starts are taken within
+// 0..T and none below one before it: no row has two tiles, and tiles are as many as prompt_tiles() says at most, whatever the starts are.
 template <class S>
 __device__ inline bool find_tile(Where &w, int &work, const PromptArgs &a, int tile, int lane)
 {
-    int before = 0;                              // tiles of the sequences seen
+    int before = 0, taken = 0;                   // tiles of the sequences seen, and where the rows of the last of them end
     bool found = false;
     work = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
@@ -104,7 +115,7 @@ __device__ inline bool find_tile(Where &w, int &work, const PromptArgs &a, int t
         int s0 = a.starts[b], s1 = a.starts[b + 1], n = a.lengths[b];
         const int room = a.width << a.page_log;
         n = n < 0 ? 0 : n > room ? room : n;
-        s0 = s0 < 0 ? 0 : s0 > a.T ? a.T : s0;
+        s0 = prompt_most_upto(s0 < taken ? taken : s0 > a.T ? a.T : s0);
         s1 = s1 < s0 ? s0 : s1 > a.T ? a.T : s1;
         const int tiles = b0 + lane < a.batch ? (int)(((int64_t)(s1 - s0) * a.group + S::Pairs - 1) / S::Pairs) : 0;
         const int upto = prompt_sums_upto(tiles);
@@ -125,6 +136,7 @@ __device__ inline bool find_tile(Where &w, int &work, const PromptArgs &a, int t
             if (a.splits == 1) return true;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
+        taken = __builtin_amdgcn_readlane(s1, 63);
     }
     return found;
 }
