@@ -66,21 +66,14 @@ __device__ inline int prompt_most_upto(int x)
 }
 // The largest of three, without the quieting of signalling NaN that fmaxf brings along (an instruction for every value).  The compiler keeps 12 states
 // between a product and the first vector instruction that takes its result, but not in front of inline assembly, whose operands it does not look at:
-// a product's result goes through largest(), which takes its first pair by fmaxf and the others behind it.
+// what goes in here is behind product_done() or behind several products more.
 __device__ inline float max3(float a, float b, float c)
 {
     float m;
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
     return m;
 }
-// `top` and pair c of a product's result; pairs are taken from the first one on.
-template <int c>
-__device__ __forceinline__ float largest(float top, const F16 &z)
-{
-    if constexpr (c == 0) return fmaxf(top, fmaxf(z[0], z[1]));
-    else return max3(top, z[2 * c], z[2 * c + 1]);
-}
-// The 12 states, where a branch lies between: there the compiler may count along the longer one of two paths that meet.
+// The 12 states.  The compiler is not relied on where a branch follows either: where two paths meet it may count along the longer one.
 __device__ __forceinline__ void product_done()
 {
     __builtin_amdgcn_sched_barrier(0);
@@ -537,7 +530,10 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
             product_done();
             finish(s, u0, p0.gone);
             float top = -INFINITY;
-            each<0, NB * 8>([&](auto two) __attribute__((always_inline)) { top = largest<two % 8>(top, s[two / 8]); });
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) top = max3(top, s[b][j], s[b][j + 1]);
             follow(top, s);
         }
         // A round has the scores of tile u.  It turns them into weights while the matrix cores compute those of u + 1, then multiplies the weights
@@ -640,7 +636,8 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
-            if constexpr (NB == 1) product_done();       // with NB of 2 the next products to be issued lie between
+            // with NB of 2 the second product has begun before the maximum takes the first block, and is half done before it takes the second
+            if constexpr (NB == 1) product_done();
             finish(next, u + 1, gone);
             float top = -INFINITY;
             {
@@ -653,7 +650,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
                     if constexpr (i < Soon) each<All - Late + i * Late / Soon, All - Late + (i + 1) * Late / Soon>(weigh);
                     each<i * All / Steps, (i + 1) * All / Steps>([&](auto two) __attribute__((always_inline)) {
                         constexpr int c = two;
-                        top = largest<c % 8>(top, next[c / 8]);
+                        top = max3(top, next[c / 8][2 * (c % 8)], next[c / 8][2 * (c % 8) + 1]);
                     });
                     if constexpr (!Copied)
                         each<i * Jobs / Steps, (i + 1) * Jobs / Steps>([&](auto job) __attribute__((always_inline)) {
