@@ -282,9 +282,9 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
     int rest = blockIdx.x / a.kv_heads;
     const int head = blockIdx.x - rest * a.kv_heads;
     if (S::Blocks == 2 && rest >= slots && all <= 2 * slots) rest = all - 1 - (rest - slots);
-    // The parts of a tile side by side where tiles are short (four drafts of 5 rows: 16.8 us, 20.0 the other way), else last what may have no share, so
-    // that the shares fill the chip evenly (prefix and cap, 256 channels: 73.5 us, 76.9).
-    const int split = S::WN > 1 ? rest % a.splits : rest / a.tiles, tile = a.tiles - 1 - (S::WN > 1 ? rest / a.splits : rest - split * a.tiles);
+    // Last what may have no share, so that the shares fill the chip evenly (prefix and cap, 256 channels: 79 us, 83 with the parts of a tile side by side;
+    // 16 sequences of 4 rows of 256 channels behind 4000 tokens 53 and 76; four drafts of 5 rows 18 either way, of 2 to 6 rows 22 and 21).
+    const int split = rest / a.tiles, tile = a.tiles - 1 - (rest - split * a.tiles);
     Where w;
     int work;
     if (!find_tile<S>(w, work, a, tile, lane)) return;
