@@ -455,7 +455,7 @@ paro_status paro_paged_attention(const paro_kv_cache *cache, const paro_half_t *
 /* The same with other scores: in place of x = scale q_h . k_t the softmax and lse take
  *      x = cap tanh(scale q_h . k_t / cap) - slopes[h] |p - t|
  * for a query at position p (here p = n - 1): scores that stay within +-cap, a bias that grows with the distance, or both.
- * A score of -inf is -cap under a cap, and its token counts.  cap: 0 (none) or positive, finite, with scale / cap finite
+ * An infinite score is cap or -cap under a cap, and its token counts.  cap: 0 (none) or positive, finite, with scale / cap finite
  * (PARO_ERR_SHAPE otherwise).  slopes: device fp32 [q_heads], 4-byte aligned, or NULL (none); finite values.  Scores are off
  * by 2^-21 of themselves at most and, with caps up to 64, by 2^-24 of the cap.  scores NULL, or with neither: paro_paged_attention. */
 typedef struct {
@@ -478,10 +478,13 @@ paro_status paro_paged_attention_scored(const paro_kv_cache *cache, const paro_h
  * rows with nothing to attend to (those at p < 0 have the prefix alone), scores, scale.  A value that is not finite makes its channel's results not finite
  * for the rows that attend to its token, whatever the weight, and for no others.  In the product with the values, weights of the softmax are off by 2^-22 of
  * themselves or 2^-35 of the row's largest; by 2^-11 in calls with neither a cap nor slopes whose heads have 64 or 128 channels and whose sequences have
- * more than 64 pairs of a row and a query head to a key-value head on average (T * q_heads > 64 kv_heads * batch), where the matrix cores are the bound.
+ * more than 64 pairs of a row and a query head to a key-value head on average (T * q_heads > 64 kv_heads * batch), where 2^-22 would take 18 to 36 % more time.
  * starts: device [batch + 1], from 0 to T and not falling (rows outside them are left as they were; a value out of range is taken as 0 or T, one
  * below another before it as that one).  T at most 2^24, q_heads at most 65535, T * q_heads + 32 kv_heads * min(batch, T) at most
  * 2^28 (a little beyond it as tiles of rows fall), table_width * page at most 2^30; otherwise PARO_ERR_UNSUPPORTED.  O nowhere in Q.
+ * Work is shared out by tiles of rows (32 to 128 pairs of a row and a query head) of every key-value head: with 512 and more of
+ * them a tile's tokens stay with one block, with n fewer at most 512 / n + 1 blocks, and 32 at most, share them.  A batch of
+ * few rows each in which one sequence is far longer than the others is faster through paro_paged_attention, a row at a time.
  * ws: >= paro_workspace_bytes_prompt() bytes, 256-byte aligned, in the two parts described at paro_workspace_bytes(); as with
  * paro_paged_attention, counters in the exchange part are zero again after every call, and blocks never wait for each other. */
 size_t paro_workspace_exchange_bytes_prompt(const paro_kv_cache *cache, int32_t q_heads, int32_t T, int32_t batch);

@@ -59,10 +59,13 @@ inline int64_t prompt_splits(int64_t tiles, int64_t kv_heads)
     return n < kMaxSplits ? n : kMaxSplits;
 }
 
-// The shapes that calls choose from, by what they have of pairs: blocks of many, whose waves have tokens of their own, or of few, whose waves share
-// them (a tile of 32 or 64 pairs is read by as many blocks less).  Sequences of 16 rows x 4 heads behind 4000 tokens take 31.1 us in the latter, 35.3 in the former,
-// of 32 rows 30.4 and 28.9.  Two blocks to a compute unit where LDS holds them: one's first and last memory accesses are the other's products (16 sequences of 4
-// rows behind 4000 tokens: 57 us, 83 with one of twice the tokens).
+// The shapes that calls choose from, by what they have of pairs: blocks of many, whose waves have pairs of their own, or of few, whose waves share
+// pairs and have tokens of their own.  8 sequences of 16 rows x 4 heads of 128 channels behind 4000 tokens take 33 us in the latter, 36 in the former,
+// of 32 rows 50 and 39; 16 sequences of 16 rows x 2 heads of 64 channels 35 and 40, of 32 rows 53 and 42; of 256 channels 56 and 69, 142 and 86.  The choice
+// is by the mean of a call's sequences and the same for all of them: 200 single rows beside a prompt of 2000 take 170 us in blocks of few, 148 in the others;
+// 15 of them beside a prompt of 4096 take 190 in blocks of many, 264 in the others.
+// Two blocks to a compute unit where LDS holds them: one's first and last memory accesses are the other's products (four drafts of 5 rows of 128
+// channels: 20 us, 28 with one of twice the tokens; 16 sequences of 4 rows behind 4000 tokens 49 either way, MXFP4 40 and 47).
 template <int D> struct Shapes;
 template <> struct Shapes<64> { typedef Shape<64, 2, 1> Many; typedef Shape<64, 1, 4> Few; };
 template <> struct Shapes<128> { typedef Shape<128, 2, 1> Many; typedef Shape<128, 1, 2> Few; };

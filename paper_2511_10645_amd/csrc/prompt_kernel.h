@@ -5,28 +5,31 @@
 // A row at position p sees an interval of tokens: [p - window + 1, p], cut at first, stretched to prefix.  Bound by the matrix
 // cores for long prompts (4 head_dim flops per row, head and token), by HBM for a few rows of a long sequence.
 //
-// A block has 128 pairs (row, query head) of one key-value head, numbered row by row, so that a head's keys and values are read once
-// for all of its query heads, and walks its tokens in tiles of 64: keys and values go through LDS as fp16 (whatever the cache
-// holds), two tiles deep, each wave of the block filling a quarter and using all for its 32 pairs.  Calls with few rows to a sequence have blocks of
-// 32 or 64 pairs whose waves share a tile's tokens instead (prompt_common.h).  A wave computes S^T = K Q^T by 32 x 32 x 16 products: a lane then has scores of one pair only, half of a tile's, so that the softmax's maximum and sum need one
-// exchange between two lanes, and S^T's registers are the B operand of O^T = V^T P^T as they are, if that product takes the tokens of a step
-// in the order 4 (lane/32) + (0..3), then 8 more; values are read from LDS transposed in that order.  The cache's order of keys (16-byte units
-// that interleave the tokens) is the first product's operand order: LDS keeps it, and no access has bank conflicts.
+// A block has 128 pairs (row, query head) of one key-value head, numbered row by row, so that a head's keys and values are read once for
+// all of its query heads, and walks its tokens in tiles of 64: keys and values go through LDS as fp16 (whatever the cache holds), two
+// tiles deep, each wave of the block filling a quarter and using all for its 32 pairs.  Calls with few rows to a sequence have blocks of
+// 32 or 64 pairs whose waves share a tile's tokens instead (prompt_common.h).  A wave computes S^T = K Q^T by 32 x 32 x 16 products: a
+// lane then has scores of one pair only, half of a tile's, so that the softmax's maximum and sum need one exchange between two lanes, and
+// S^T's registers are the B operand of O^T = V^T P^T as they are, if that product takes the tokens of a step in the order 4 (lane/32) +
+// (0..3), then 8 more; values are read from LDS transposed in that order.  The cache's order of keys (16-byte units that interleave the
+// tokens) is the first product's operand order: LDS keeps it, and no access has bank conflicts.
 //
-// p enters the second product as fp16 numbers after a factor of 2^kShift (16 bits would otherwise end at 2^-24 of the maximum): as two, p and
-// what its rounding left, which together are off by 2^-22 of p or by 2^-35 of the largest, where that product is not what the time goes into:
-// blocks for few rows (0 to 6 % over fp16 caches, 6 to 13 % over others), heads of 256 channels (8 to 13 %), scores with a cap or a bias (8 to 14 %).
-// Otherwise as one, off by 2^-11 of itself at most, independently, which adds about as much to a result as its own rounding to fp16 (2.9e-4 of
-// the 2-norm instead of 2.0e-4): a second one costs 512 rows behind 32256 tokens 375 us instead of 280, 8192 rows 725 instead of 534, 2048 rows
-// 65 instead of 53 (E4M3 71 and 58, MXFP4 69 and 58), 8 x 1024 rows of heads of 64 93 instead of 77.  Sums stay in fp32.
+// p enters the second product as fp16 numbers after a factor of 2^kShift (16 bits would otherwise end at 2^-24 of the maximum): as two, p
+// and what its rounding left, which together are off by 2^-22 of p or by 2^-35 of the largest, where that product is not what the time
+// goes into: blocks for few rows (0 to 6 % over fp16 caches, 6 to 13 % over others), heads of 256 channels (8 to 13 %), scores with a cap
+// or a bias (8 to 14 %). Otherwise as one, off by 2^-11 of itself at most, independently, which adds about as much to a result as its own
+// rounding to fp16 (2.9e-4 of the 2-norm instead of 2.0e-4): a second one costs 512 rows behind 32256 tokens 375 us instead of 280, 8192
+// rows 725 instead of 534, 2048 rows 65 instead of 53 (E4M3 71 and 58, MXFP4 69 and 58), 8 x 1024 rows of heads of 64 93 instead of 77.
+// Sums stay in fp32.
 //
 // Few tiles with long sequences: `splits` blocks share a tile's tokens; each leaves fp32 results in the scratch, and the one that arrives
 // last joins all in their order, so that results do not depend on timing.  Nobody waits.
 //
-// Measured (32 query and 8 key-value heads of 128 channels, fp16): 512 rows behind 32256 tokens 277 us (985 TFLOP/s; 1180 is what a large fp16 product of random
-// numbers reaches on the card, whose clock falls to 1.5 GHz under either), 8192 rows alone 552 (996), 2048 rows alone 50 (687).  A round of a wave takes 2600 cycles
-// alone and 3200 beside another, 1024 of them products: both waves of a SIMD need its vector unit for 1100 each (exponentials 8 cycles, products' issue 8,
-// others 4).  What a block has besides: 11000 cycles to its first scores (arguments, starts, pages and keys are memory's latency one after the other), 8000 from the last.
+// Measured (32 query and 8 key-value heads of 128 channels, fp16): 512 rows behind 32256 tokens 280 us (975 TFLOP/s; 1180 is what a large
+// fp16 product of random numbers reaches on the card, whose clock falls to 1.5 GHz under either), 8192 rows alone 560 (980), 2048 rows
+// alone 50 (685).  A round of a wave takes 2600 cycles alone and 3200 beside another, 1024 of them products: both waves of a SIMD need
+// its vector unit for 1100 each (exponentials 8 cycles, products' issue 8, others 4).  What a block has besides: 11000 cycles to its
+// first scores (arguments, starts, pages and keys are memory's latency one after the other), 8000 from the last.
 #pragma once
 
 #include <type_traits>
@@ -540,7 +543,7 @@ __global__ __launch_bounds__(kPromptThreads, S::Blocks) void prompt_attention_ke
         // with the values of u while it looks for the next maximum; keys of u + 2 and values of u + 1 go to LDS meanwhile.  What the vector units do is dealt
         // out over the matrix instructions evenly, 32 cycles of a matrix core to as many of a vector unit: 8 each for the issue and for an exponential, 4 for others.
         const auto round = [&](int u, uint8_t *free_keys, uint8_t *keys, uint8_t *values, uint8_t *free_values) __attribute__((always_inline)) {
-            // operands on their way from LDS, which takes 130 cycles and more; fewer where registers are short (prefix and cap, 256 channels: 72.2 us, 73.4 with 5)
+            // operands on their way from LDS, which takes 130 cycles and more; fewer where registers are short (2048 rows, cap, E4M3: 101 us, 130 with 5)
             constexpr int Ahead = SCORED ? 3 : NB * KS < 5 ? NB * KS : 5;
             half8v f[Ahead + 1];
             each<0, Ahead>([&](auto at) __attribute__((always_inline)) { f[at] = key_frag(keys, at); });
