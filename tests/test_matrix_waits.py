@@ -1,7 +1,7 @@
-"""No vector instruction of the built kernels comes too soon behind the matrix instruction whose result it takes.
+"""No vector or memory instruction of the built kernels comes too soon behind the matrix instruction whose result it takes.
 
 The compiler puts idle states in between, but not in front of inline assembly, whose operands it does not look at.  Here the library's own machine code is
-read: along every path from a 32x32x16 or 16x16x32 product of fp16 numbers to the first vector instruction that touches its result there are as many
+read: along every path from a 32x32x16 or 16x16x32 product of fp16 numbers to the first such instruction that touches its result there are as many
 states as the compiler keeps between the two where it sees both.  No GPU is needed."""
 import re
 import struct
@@ -49,12 +49,12 @@ def kernels(listing):
 
 
 def too_soon(code, states=STATES):
-    """[(address, instruction, states)] of vector instructions that come sooner than that behind the product whose result they touch."""
+    """[(address, instruction, states)] of instructions that come sooner than that behind the product whose result they touch."""
     at = {a: i for i, (a, *_) in enumerate(code)}
     leaders = sorted({0} | {at[t] for *_, t in code if t is not None} | {i + 1 for i, (_, op, *_) in enumerate(code) if "branch" in op or op == "s_endpgm"})
     leaders = [x for x in leaders if x < len(code)]
     ends = dict(zip(leaders, leaders[1:] + [len(code)]))
-    needs = [registers(ops) if op.startswith("v_") else None for _, op, ops, _ in code]
+    needs = [registers(ops) if op.startswith(("v_", "ds_", "buffer_", "global_", "scratch_")) else None for _, op, ops, _ in code]
     found, before, work = {}, {0: {}}, [0]
     while work:
         start = work.pop()
